@@ -31,7 +31,11 @@
  *                            the N strings of highest plug-in score
  *                            prod_j q_j(y_j) over the drafter's marginals
  *                            (Assumption 1, Sec. 3.2; Sec. 3.3), as parent
- *                            and token arrays ready for tree verification.
+ *                            and token arrays ready for tree verification;
+ *   glance_cache_*           the same attention and commit over a context cache
+ *                            that is read in part (a window and its first
+ *                            tokens), held in 4 bits or shortened by the
+ *                            attention weight its slots received.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -335,6 +339,146 @@ glance_status glance_build_tree(int32_t batch, int32_t horizon, int32_t vocab, i
                                 glance_dtype logits_dtype, const void* draft_logits, int64_t seq_stride,
                                 const int32_t* roots, int32_t* parents, int32_t* tokens, float* scores,
                                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * ---- Context caches ------------------------------------------------------
+ * A context cache as an object: keys and values of each sequence's context,
+ * dense or in 4 bits, with its lengths and, for eviction, the attention weight
+ * that each slot has received.
+ *
+ *   batch, n_kv_heads, head_dim (64 or 128), capacity (0..2^25 slots)
+ *   format      GLANCE_CACHE_DENSE: k, v device [batch][Hkv][capacity][D] of
+ *               `dtype`.  GLANCE_CACHE_KV4: k, v device
+ *               [batch][Hkv][capacity][D/2] bytes, two 4-bit codes each (the
+ *               even dim in the low half), and k_scale, v_scale device
+ *               [batch][Hkv][capacity][D/32] bytes; dtype is not read.
+ *   ctx_lens    device [batch] int32, slots in use per sequence (clamped to
+ *               [0, capacity] where read)
+ *   weights     device [batch][Hkv][capacity] float32, or NULL where no call
+ *               that needs them is made
+ * k, v and the scales are 16-byte aligned.  Slots at or past ctx_lens are never
+ * read, except that rows committed or weighed go there.
+ *
+ * 4-bit values: 32 consecutive dims of a key (or value) share a power of two
+ * 2^e and each is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e (codes
+ * 0..7, plus 8 for the sign), ties to the even code, at most 6.  With a the
+ * block's largest magnitude, e = floor(log2 a) - 2, one more if
+ * a >= 1.75 * 2^floor(log2 a), and within -125..125; a block of zeros has
+ * e = -125.  The scale byte is e + 127; 255 marks a block that held a NaN or an
+ * infinity, whose values all read as NaN (codes unspecified).
+ *
+ * Visibility.  Calls that read a cache take n_sinks and window (0: no window,
+ * and n_sinks is not used).  With a window, the row at position p sees the
+ * context slot j iff j < n_sinks or p - j < window; slot j's position is j.
+ * Row i of a block is at position ctx + i, a tree's node at ctx + its depth.
+ * Of the new keys a block's rows see all (the block stays bidirectional within
+ * itself), a tree's rows see their ancestors at positions that satisfy the same
+ * condition, and every row sees itself.  Context that no row of a call sees is
+ * not read, whatever it holds.  A key or value that some row sees has to be
+ * finite: a NaN or infinity in it may reach other rows of the same sequence and
+ * KV head.
+ */
+typedef enum { GLANCE_CACHE_DENSE = 0, GLANCE_CACHE_KV4 = 1 } glance_cache_format;
+
+typedef struct {
+  int32_t batch;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t capacity;
+  glance_cache_format format;
+  glance_dtype dtype;
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+  int32_t* ctx_lens;
+  float* weights;
+} glance_cache;
+
+/*
+ * glance_block_draft_attn and glance_tree_verify_attn over a cache: the same
+ * rows, outputs and conventions.  batch, n_kv_heads, head_dim and capacity of
+ * the cache must be the shape's, and a dense cache's dtype too; over a 4-bit
+ * cache q, k_new, v_new and out are of s->dtype, the keys and values being the
+ * exact values of their codes.  The call with n_new = 1 is one decoding step.
+ *   workspace   >= glance_cache_attn_workspace_size(s, n_sinks, window) bytes
+ */
+glance_status glance_cache_block_draft_attn(const glance_attn_shape* s, const glance_cache* cache, int32_t n_sinks,
+                                            int32_t window, const void* q, const void* k_new, const void* v_new,
+                                            void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                            hipStream_t stream);
+glance_status glance_cache_tree_verify_attn(const glance_attn_shape* s, const glance_cache* cache, int32_t n_sinks,
+                                            int32_t window, const void* q, const void* k_new, const void* v_new,
+                                            const int32_t* parents, void* out, float* lse, void* workspace,
+                                            size_t workspace_bytes, hipStream_t stream);
+
+/* Workspace bytes of the two calls above (0 if an argument is invalid). Host only. */
+size_t glance_cache_attn_workspace_size(const glance_attn_shape* s, int32_t n_sinks, int32_t window);
+
+/*
+ * The keys and values of src's slots in the format of dst: one of the two is
+ * dense and the other in 4 bits (a prefilled cache goes into 4 bits; a 4-bit
+ * one comes back as the values it stands for, exactly).  Slots below
+ * min(src length, dst capacity) are written, and dst's lengths set to that;
+ * weights stay as they are.  src and dst must not overlap; the two may share
+ * ctx_lens.
+ */
+glance_status glance_cache_convert(const glance_cache* src, const glance_cache* dst, hipStream_t stream);
+
+/*
+ * glance_commit_path into a cache: the accepted rows of k_new, v_new (device
+ * [batch][n_nodes][Hkv][D] of `dtype`, 16-byte aligned for a 4-bit cache; for
+ * a dense one dtype must be the cache's) go into slots ctx..ctx + a, rounded
+ * to 4 bits for a 4-bit cache, and ctx_lens advances.  Clamps as there.
+ */
+glance_status glance_cache_commit_path(const glance_cache* cache, int32_t n_nodes, glance_dtype dtype,
+                                       const void* k_new, const void* v_new, const int32_t* accept_len,
+                                       const int32_t* accept_path, int32_t path_stride, hipStream_t stream);
+
+/*
+ * Attention weight received by each context slot, accumulated: for every slot
+ * j < ctx of every sequence b and KV head g
+ *     weights_out[b,g,j] = decay * weights[b,g,j]
+ *                        + sum_(i,h) exp(sm_scale * q[b,i,h] . key_j - lse[b,i,h])
+ * over the query heads h of g and those rows i that see slot j.
+ *   q, lse      of an attention call over this cache with the same shape,
+ *               n_sinks and window: device [batch][n_new][Hq][D] s->dtype, and
+ *               its log-sum-exps
+ *   accept_path NULL: the rows are all n_new rows of a block, row i at position
+ *               ctx + i; k_new and accept_len are NULL too.  Otherwise
+ *               accept_len and accept_path are an acceptance's outputs, the
+ *               rows are the path's nodes (as many as glance_commit_path
+ *               would commit), the t-th at position ctx + t, and slot ctx + t,
+ *               which its key (of k_new, device [batch][n_new][Hkv][D]) is about to
+ *               take, gets the weight it received from the path's rows t.. (no
+ *               old value enters).  Call it before the commit.
+ *   decay       in [0, 1]; 0 reads no old weights (cache->weights may be NULL)
+ *   weights_out device [batch][Hkv][capacity] float32: cache->weights itself or a
+ *               buffer apart from it; other slots are left as they are
+ * Sums are fp32, in a fixed order: the same inputs give the same bits.
+ */
+glance_status glance_cache_weigh(const glance_attn_shape* s, const glance_cache* cache, int32_t n_sinks,
+                                 int32_t window, const void* q, const float* lse, const void* k_new,
+                                 const int32_t* accept_len, const int32_t* accept_path, int32_t path_stride,
+                                 float decay, float* weights_out, hipStream_t stream);
+
+/*
+ * Eviction: for every sequence and KV head the slots to keep, copied in order
+ * into another cache of the same format.  A sequence of at most `budget` slots
+ * is kept whole.  Of a longer one the first n_sinks, the last n_recent and, of
+ * the others, the budget - n_sinks - n_recent of greatest weight are kept; ties
+ * go to the lowest slot, and a NaN weight counts as larger than every number.
+ *   budget      1..dst's capacity; n_sinks + n_recent <= budget
+ *   dst         K, V, scales and weights of slots below min(length, budget) are
+ *               written, the others left as they are; ctx_lens becomes that
+ *               minimum (src's may be the same array).  No other buffer may
+ *               overlap src's.
+ *   kept        device [batch][Hkv][budget] int32: the source slot of each kept
+ *               one, then -1
+ * batch * n_kv_heads <= 65535.  No workspace.
+ */
+glance_status glance_cache_evict(const glance_cache* src, const glance_cache* dst, int32_t budget, int32_t n_sinks,
+                                 int32_t n_recent, int32_t* kept, hipStream_t stream);
 
 /* Workspace bytes glance_build_tree needs (0 if the sizes are invalid). Host only. */
 size_t glance_tree_workspace_size(int32_t batch, int32_t horizon, int32_t vocab, int32_t budget);

@@ -22,8 +22,9 @@ the GPU path:
 * ``tree``       -- the tree builder of Sec. 3.3 (Algorithm 1, second step): the
   N strings of highest plug-in score prod_j q_j(y_j) (Assumption 1) packed as
   a prefix-closed tree, by exhaustive and by best-first enumeration;
+* ``cache``      -- a context cache read in part, in 4 bits, weighed and evicted;
 * ``tiny_model`` -- a tiny random-weight float64 decoder used to check the
   lossless greedy equivalence of Thm. 1 (Sec. 3.3, App. A.1).
 """
 
-from . import attention, accept, commit, sampling, tiny_model, tree  # noqa: F401
+from . import accept, attention, cache, commit, sampling, tiny_model, tree  # noqa: F401

@@ -16,6 +16,15 @@ missing or a GPU is absent, the calls raise.
     glance_build_tree(draft_logits, roots, budget) -> dict(parents, tokens, scores)
     glance_commit_path(k_new, v_new, accept_len, accept_path, k_ctx, v_ctx, ctx_lens)  (in place)
 
+and over a ContextCache (dense or in 4 bits, with lengths and slot weights; new_cache allocates one):
+
+    glance_cache_block_draft_attn(q, cache, k_new, v_new, n_sinks, window) -> (out, lse)
+    glance_cache_tree_verify_attn(q, cache, k_new, v_new, parents, n_sinks, window) -> (out, lse)
+    glance_cache_convert(src, dst)                                            (dense <-> 4 bits)
+    glance_cache_commit_path(cache, k_new, v_new, accept_len, accept_path)    (in place)
+    glance_cache_weigh(q, cache, lse, k_new, accept_len, accept_path, decay) -> weights
+    glance_cache_evict(src, dst, budget, n_sinks, n_recent) -> kept
+
 Layouts: q, out [batch][n][Hq][D]; k_ctx, v_ctx [batch][Hkv][capacity][D];
 k_new, v_new [batch][n][Hkv][D]; ctx_lens [batch] int32; parents, tokens
 [batch][n] int32; logits [batch][n][vocab]; draft_logits [batch][rows][vocab]
@@ -31,6 +40,7 @@ LIB_PATH = os.path.join(_HERE, "libglance.so")
 GLANCE_OK, GLANCE_ERR_INVALID_ARG, GLANCE_ERR_UNSUPPORTED, GLANCE_ERR_WORKSPACE, GLANCE_ERR_HIP = \
     0, -1, -2, -3, -4
 GLANCE_F32, GLANCE_BF16 = 0, 1
+GLANCE_CACHE_DENSE, GLANCE_CACHE_KV4 = 0, 1
 
 
 class GlanceError(RuntimeError):
@@ -46,8 +56,17 @@ class AttnShape(ctypes.Structure):
                 ("dtype", ctypes.c_int)]
 
 
+class CacheStruct(ctypes.Structure):
+    """glance_cache of include/glance.h."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("format", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p), ("weights", ctypes.c_void_p)]
+
+
 _lib = None
 _P = ctypes.c_void_p
+_CACHE = ctypes.POINTER(CacheStruct)
 _I32 = ctypes.c_int32
 _SZ = ctypes.c_size_t
 
@@ -70,6 +89,16 @@ _SIGS = {
     "glance_tree_workspace_size": (_SZ, [_I32, _I32, _I32, _I32]),
     "glance_commit_path": (ctypes.c_int, [_I32, _I32, _I32, _I32, _I32, ctypes.c_int, _P, _P, _P, _P, _I32, _P,
                                           _P, _P, _P]),
+    "glance_cache_block_draft_attn": (ctypes.c_int, [ctypes.POINTER(AttnShape), _CACHE, _I32, _I32, _P, _P, _P, _P,
+                                                     _P, _P, _SZ, _P]),
+    "glance_cache_tree_verify_attn": (ctypes.c_int, [ctypes.POINTER(AttnShape), _CACHE, _I32, _I32, _P, _P, _P, _P,
+                                                     _P, _P, _P, _SZ, _P]),
+    "glance_cache_attn_workspace_size": (_SZ, [ctypes.POINTER(AttnShape), _I32, _I32]),
+    "glance_cache_convert": (ctypes.c_int, [_CACHE, _CACHE, _P]),
+    "glance_cache_commit_path": (ctypes.c_int, [_CACHE, _I32, ctypes.c_int, _P, _P, _P, _P, _I32, _P]),
+    "glance_cache_weigh": (ctypes.c_int, [ctypes.POINTER(AttnShape), _CACHE, _I32, _I32, _P, _P, _P, _P, _P, _I32,
+                                          ctypes.c_float, _P, _P]),
+    "glance_cache_evict": (ctypes.c_int, [_CACHE, _CACHE, _I32, _I32, _I32, _P, _P]),
     "glance_attn_workspace_size": (_SZ, [ctypes.POINTER(AttnShape), ctypes.c_int]),
     "glance_accept_workspace_size": (_SZ, [_I32, _I32, _I32]),
     "glance_validate_tree": (ctypes.c_int, [_I32, _P, _P, _I32]),
@@ -453,6 +482,290 @@ def glance_commit_path(k_new, v_new, accept_len, accept_path, k_ctx, v_ctx, ctx_
                                                   ctx_lens, stream)))
 
 
+# ---------------------------------------------------------------- context caches
+class ContextCache:
+    """A context cache: each sequence's keys and values, lengths and slot weights.
+
+    k, v      dense: [batch][Hkv][capacity][D] float32 or bfloat16; in 4 bits:
+              [batch][Hkv][capacity][D / 2] uint8 with k_scale, v_scale
+              [batch][Hkv][capacity][D / 32] uint8
+    ctx_lens  [batch] int32
+    weights   [batch][Hkv][capacity] float32, or None (weighing and eviction need them)
+    """
+
+    def __init__(self, k, v, ctx_lens, k_scale=None, v_scale=None, weights=None):
+        self.k, self.v, self.ctx_lens = k, v, ctx_lens
+        self.k_scale, self.v_scale, self.weights = k_scale, v_scale, weights
+
+    @property
+    def kv4(self):
+        return self.k_scale is not None
+
+    @property
+    def batch(self):
+        return self.k.shape[0]
+
+    @property
+    def n_kv_heads(self):
+        return self.k.shape[1]
+
+    @property
+    def capacity(self):
+        return self.k.shape[2]
+
+    @property
+    def head_dim(self):
+        return self.k.shape[3] * (2 if self.kv4 else 1)
+
+
+def new_cache(batch, n_kv_heads, capacity, head_dim, dtype=None, fmt="dense", weights=False, device="cuda"):
+    """An empty ContextCache (zeroed; fmt "dense" or "kv4"; dtype bfloat16 by default, of a dense cache)."""
+    torch = _torch()
+    if fmt not in ("dense", "kv4"):
+        raise ValueError(f'fmt must be "dense" or "kv4", got {fmt!r}')
+
+    def zeros(width, dt):
+        return torch.zeros((batch, n_kv_heads, capacity, width), dtype=dt, device=device)
+
+    lens = torch.zeros((batch,), dtype=torch.int32, device=device)
+    w = torch.zeros((batch, n_kv_heads, capacity), dtype=torch.float32, device=device) if weights else None
+    if fmt == "kv4":
+        if head_dim % 32:
+            raise ValueError(f"head_dim must be a multiple of 32, got {head_dim}")
+        u8 = torch.uint8
+        return ContextCache(zeros(head_dim // 2, u8), zeros(head_dim // 2, u8), lens, zeros(head_dim // 32, u8),
+                            zeros(head_dim // 32, u8), w)
+    dt = dtype or torch.bfloat16
+    return ContextCache(zeros(head_dim, dt), zeros(head_dim, dt), lens, weights=w)
+
+
+def _same_device(*tensors):
+    """The calls run on the current device's stream: every tensor has to be there."""
+    torch = _torch()
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{here}")
+
+
+def _cache_struct(cache, name):
+    """The C view of a ContextCache, its tensors checked."""
+    torch = _torch()
+    kv4 = cache.kv4
+    if kv4 != (cache.v_scale is not None):
+        raise ValueError(f"{name}: k_scale and v_scale go together")
+    _dev(cache.k, f"{name}.k", torch.uint8 if kv4 else None, 4)
+    _dev(cache.v, f"{name}.v", cache.k.dtype, 4)
+    if tuple(cache.v.shape) != tuple(cache.k.shape):
+        raise ValueError(f"{name}.v must match {name}.k")
+    batch, hkv, cap, d = cache.batch, cache.n_kv_heads, cache.capacity, cache.head_dim
+    for t, what, shape, dt in ((cache.k_scale, "k_scale", (batch, hkv, cap, d // 32), torch.uint8),
+                               (cache.v_scale, "v_scale", (batch, hkv, cap, d // 32), torch.uint8),
+                               (cache.ctx_lens, "ctx_lens", (batch,), torch.int32),
+                               (cache.weights, "weights", (batch, hkv, cap), torch.float32)):
+        if t is not None:
+            _dev(t, f"{name}.{what}", dt)
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name}.{what} must have shape {shape}, got {tuple(t.shape)}")
+    if cache.ctx_lens is None:
+        raise ValueError(f"{name}.ctx_lens is missing")
+    _same_device(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.ctx_lens, cache.weights)
+    return CacheStruct(batch, hkv, d, cap, GLANCE_CACHE_KV4 if kv4 else GLANCE_CACHE_DENSE,
+                       GLANCE_F32 if kv4 else _dtype_code(cache.k), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_scale),
+                       _ptr(cache.v_scale), _ptr(cache.ctx_lens), _ptr(cache.weights))
+
+
+def _cache_query(q, cache, sm_scale):
+    """Checks of the queries against the cache, and the call's shape."""
+    _dev(q, "q", ndim=4)
+    code = _dtype_code(q)
+    batch, n, hq, d = q.shape
+    if batch != cache.batch or d != cache.head_dim:
+        raise ValueError("q must be [batch][n][Hq][D] with the cache's batch and D")
+    if not cache.kv4 and cache.k.dtype != q.dtype:
+        raise TypeError(f"a dense cache must have q's dtype, got {cache.k.dtype} and {q.dtype}")
+    return attn_shape(batch, n, hq, cache.n_kv_heads, d, cache.capacity, code, sm_scale)
+
+
+def _new_rows(t, name, q, cache):
+    _dev(t, name, q.dtype, 4)
+    want = (q.shape[0], q.shape[1], cache.n_kv_heads, q.shape[3])
+    if tuple(t.shape) != want:
+        raise ValueError(f"{name} must be [batch][n][Hkv][D] = {want}, got {tuple(t.shape)}")
+
+
+def _path_args(accept_len, accept_path, batch):
+    torch = _torch()
+    _dev(accept_len, "accept_len", torch.int32, 1)
+    _dev(accept_path, "accept_path", torch.int32, 2)
+    if accept_len.shape[0] != batch or accept_path.shape[0] != batch:
+        raise ValueError("accept_len and accept_path need one row per sequence")
+    return accept_path.shape[1]
+
+
+def glance_cache_attn_workspace_size(shape, n_sinks=0, window=0):
+    return int(lib().glance_cache_attn_workspace_size(ctypes.byref(shape), int(n_sinks), int(window)))
+
+
+def _cache_attn_args(tree, q, cache, k_new, v_new, parents, n_sinks, window, out, lse, workspace, sm_scale, stream,
+                     want_lse):
+    torch = _torch()
+    shape = _cache_query(q, cache, sm_scale)
+    _new_rows(k_new, "k_new", q, cache)
+    _new_rows(v_new, "v_new", q, cache)
+    view = _cache_struct(cache, "cache")
+    if tree:
+        _dev(parents, "parents", torch.int32, 2)
+        if tuple(parents.shape) != tuple(q.shape[:2]):
+            raise ValueError("parents must be [batch][n]")
+    if out is None:
+        out = _new_output(torch.empty_like, q, stream)
+    else:
+        _dev(out, "out", q.dtype, 4)
+        if tuple(out.shape) != tuple(q.shape):
+            raise ValueError("out must match q")
+    if lse is None and want_lse:
+        lse = _new_output(torch.empty, tuple(q.shape[:3]), stream, dtype=torch.float32, device=q.device)
+    elif lse is not None:
+        _dev(lse, "lse", torch.float32, 3)
+        if tuple(lse.shape) != tuple(q.shape[:3]):
+            raise ValueError("lse must be [batch][n][Hq]")
+    _same_device(q, k_new, v_new, parents, out, lse, workspace)
+    need = glance_cache_attn_workspace_size(shape, n_sinks, window)
+    if need == 0:
+        raise GlanceError(GLANCE_ERR_INVALID_ARG, glance_last_error())
+    ws = _workspace(need, q.device, workspace, stream)
+    args = [ctypes.byref(shape), ctypes.byref(view), int(n_sinks), int(window), _ptr(q), _ptr(k_new), _ptr(v_new)]
+    if tree:
+        args += [_ptr(parents)]
+    args += [_ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)]
+    fn = lib().glance_cache_tree_verify_attn if tree else lib().glance_cache_block_draft_attn
+    # the tensors, not the cache: a prepared call keeps what its pointers name
+    keep = (shape, view, q, k_new, v_new, parents, out, lse, ws) + _cache_tensors(cache)
+    return fn, args, out, lse, keep
+
+
+def _cache_tensors(cache):
+    return (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.ctx_lens, cache.weights)
+
+
+def glance_cache_block_draft_attn(q, cache, k_new, v_new, n_sinks=0, window=0, out=None, lse=None, workspace=None,
+                                  sm_scale=0.0, stream=None, want_lse=True):
+    """Block-draft attention over a cache (n = 1: a decoding step).  With window > 0 a row sees
+    the last `window` positions up to its own and the first n_sinks slots.  Returns (out, lse)."""
+    fn, args, out, lse, _ = _cache_attn_args(False, q, cache, k_new, v_new, None, n_sinks, window, out, lse, workspace,
+                                             sm_scale, stream, want_lse)
+    _check(fn(*args))
+    return out, lse
+
+
+def glance_cache_tree_verify_attn(q, cache, k_new, v_new, parents, n_sinks=0, window=0, out=None, lse=None,
+                                  workspace=None, sm_scale=0.0, stream=None, want_lse=True):
+    """Ancestor-masked tree-verify attention over a cache; window and sinks also bound which
+    ancestors a node sees.  Returns (out, lse)."""
+    fn, args, out, lse, _ = _cache_attn_args(True, q, cache, k_new, v_new, parents, n_sinks, window, out, lse,
+                                             workspace, sm_scale, stream, want_lse)
+    _check(fn(*args))
+    return out, lse
+
+
+def _convert_args(src, dst, stream):
+    a, b = _cache_struct(src, "src"), _cache_struct(dst, "dst")
+    return ([ctypes.byref(a), ctypes.byref(b), _stream(stream)],
+            (a, b) + _cache_tensors(src) + _cache_tensors(dst))
+
+
+def glance_cache_convert(src, dst, stream=None):
+    """src's keys and values in dst's format (one dense, the other in 4 bits); sets dst.ctx_lens."""
+    _check(lib().glance_cache_convert(*_convert_args(src, dst, stream)[0]))
+
+
+def glance_cache_commit_path(cache, k_new, v_new, accept_len, accept_path, stream=None):
+    """Append the accepted path's key/value rows to the cache (rounded to 4 bits where it is held
+    so) and advance its lengths, in place."""
+    view = _cache_struct(cache, "cache")
+    _dev(k_new, "k_new", ndim=4)
+    code = _dtype_code(k_new)
+    if not cache.kv4 and cache.k.dtype != k_new.dtype:
+        raise TypeError(f"a dense cache must have k_new's dtype, got {cache.k.dtype} and {k_new.dtype}")
+    _dev(v_new, "v_new", k_new.dtype, 4)
+    n = k_new.shape[1]
+    want = (cache.batch, n, cache.n_kv_heads, cache.head_dim)
+    if tuple(k_new.shape) != want or tuple(v_new.shape) != want:
+        raise ValueError(f"k_new / v_new must be [batch][n][Hkv][D] = {want}")
+    stride = _path_args(accept_len, accept_path, cache.batch)
+    _same_device(k_new, v_new, accept_len, accept_path)
+    _check(lib().glance_cache_commit_path(ctypes.byref(view), n, code, _ptr(k_new), _ptr(v_new), _ptr(accept_len),
+                                          _ptr(accept_path), stride, _stream(stream)))
+
+
+def _weigh_args(q, cache, lse, k_new, accept_len, accept_path, decay, n_sinks, window, weights_out, sm_scale, stream):
+    torch = _torch()
+    shape = _cache_query(q, cache, sm_scale)
+    view = _cache_struct(cache, "cache")
+    _dev(lse, "lse", torch.float32, 3)
+    if tuple(lse.shape) != tuple(q.shape[:3]):
+        raise ValueError("lse must be [batch][n][Hq]")
+    stride = 0
+    if accept_path is not None:
+        if k_new is None or accept_len is None:
+            raise ValueError("a path needs k_new, accept_len and accept_path")
+        _new_rows(k_new, "k_new", q, cache)
+        stride = _path_args(accept_len, accept_path, q.shape[0])
+    elif k_new is not None or accept_len is not None:
+        raise ValueError("k_new and accept_len belong to a path")
+    if weights_out is None:
+        weights_out = cache.weights
+        if weights_out is None:
+            raise ValueError("the cache has no weights, and no weights_out is given")
+    _dev(weights_out, "weights_out", torch.float32, 3)
+    want = (cache.batch, cache.n_kv_heads, cache.capacity)
+    if tuple(weights_out.shape) != want:
+        raise ValueError(f"weights_out must be [batch][Hkv][capacity] = {want}")
+    _same_device(q, lse, k_new, accept_len, accept_path, weights_out)
+    args = [ctypes.byref(shape), ctypes.byref(view), int(n_sinks), int(window), _ptr(q), _ptr(lse), _ptr(k_new),
+            _ptr(accept_len), _ptr(accept_path), stride, float(decay), _ptr(weights_out), _stream(stream)]
+    keep = (shape, view, q, lse, k_new, accept_len, accept_path, weights_out) + _cache_tensors(cache)
+    return args, weights_out, keep
+
+
+def glance_cache_weigh(q, cache, lse, k_new=None, accept_len=None, accept_path=None, decay=1.0, n_sinks=0, window=0,
+                       weights_out=None, sm_scale=0.0, stream=None):
+    """Add to each slot's weight the attention it received in a call with these queries and
+    log-sum-exps: of every row of a block, or (accept_len, accept_path and k_new given) of an
+    accepted path's rows, whose own slots-to-be get theirs.  Old weights count `decay` times.
+    Writes weights_out (cache.weights by default) and returns it."""
+    args, weights_out, _ = _weigh_args(q, cache, lse, k_new, accept_len, accept_path, decay, n_sinks, window,
+                                       weights_out, sm_scale, stream)
+    _check(lib().glance_cache_weigh(*args))
+    return weights_out
+
+
+def _evict_args(src, dst, budget, n_sinks, n_recent, kept, stream):
+    torch = _torch()
+    a, b = _cache_struct(src, "src"), _cache_struct(dst, "dst")
+    shape = (src.batch, src.n_kv_heads, int(budget))
+    if kept is None:
+        if budget < 1:
+            raise ValueError(f"budget must be >= 1, got {budget}")
+        kept = _new_output(torch.empty, shape, stream, dtype=torch.int32, device=src.k.device)
+    _dev(kept, "kept", torch.int32, 3)
+    if tuple(kept.shape) != shape:
+        raise ValueError(f"kept must be [batch][Hkv][budget] = {shape}")
+    _same_device(kept)
+    args = [ctypes.byref(a), ctypes.byref(b), int(budget), int(n_sinks), int(n_recent), _ptr(kept), _stream(stream)]
+    return args, kept, (a, b, kept) + _cache_tensors(src) + _cache_tensors(dst)
+
+
+def glance_cache_evict(src, dst, budget, n_sinks=0, n_recent=0, kept=None, stream=None):
+    """Keep `budget` slots of every longer sequence, per KV head: the first n_sinks, the last
+    n_recent and those of greatest weight, copied in order into dst (same format, its lengths
+    set).  Returns kept [batch][Hkv][budget] int32, the source slots (-1 past the last)."""
+    args, kept, _ = _evict_args(src, dst, budget, n_sinks, n_recent, kept, stream)
+    _check(lib().glance_cache_evict(*args))
+    return kept
+
+
 # ---------------------------------------------------------------- prepared calls
 class PreparedCall:
     """A library call with all arguments checked and marshalled once.
@@ -531,3 +844,40 @@ def prepare_build_tree(draft_logits, roots, budget, first_row=0, horizon=None, o
     _check(lib().glance_build_tree(*args))
     keep = (draft_logits, roots, outputs, ws)
     return PreparedCall(lib().glance_build_tree, args, keep), outputs
+
+
+# The prepared calls on caches check and marshal, and run nothing until called.
+def prepare_cache_block_draft_attn(q, cache, k_new, v_new, n_sinks=0, window=0, out=None, lse=None, workspace=None,
+                                   sm_scale=0.0, stream=None):
+    """Returns (call, out, lse): call() runs the draft attention over the cache into out / lse."""
+    fn, args, out, lse, keep = _cache_attn_args(False, q, cache, k_new, v_new, None, n_sinks, window, out, lse,
+                                                workspace, sm_scale, stream, lse is not None)
+    return PreparedCall(fn, args, keep), out, lse
+
+
+def prepare_cache_tree_verify_attn(q, cache, k_new, v_new, parents, n_sinks=0, window=0, out=None, lse=None,
+                                   workspace=None, sm_scale=0.0, stream=None):
+    """Returns (call, out, lse): call() runs the tree-verify attention over the cache into out / lse."""
+    fn, args, out, lse, keep = _cache_attn_args(True, q, cache, k_new, v_new, parents, n_sinks, window, out, lse,
+                                                workspace, sm_scale, stream, lse is not None)
+    return PreparedCall(fn, args, keep), out, lse
+
+
+def prepare_cache_convert(src, dst, stream=None):
+    """Returns call: call() converts src into dst."""
+    args, keep = _convert_args(src, dst, stream)
+    return PreparedCall(lib().glance_cache_convert, args, keep)
+
+
+def prepare_cache_weigh(q, cache, lse, k_new=None, accept_len=None, accept_path=None, decay=1.0, n_sinks=0, window=0,
+                        weights_out=None, sm_scale=0.0, stream=None):
+    """Returns call: call() accumulates the weights into weights_out (cache.weights by default)."""
+    args, _, keep = _weigh_args(q, cache, lse, k_new, accept_len, accept_path, decay, n_sinks, window, weights_out,
+                                sm_scale, stream)
+    return PreparedCall(lib().glance_cache_weigh, args, keep)
+
+
+def prepare_cache_evict(src, dst, budget, n_sinks=0, n_recent=0, kept=None, stream=None):
+    """Returns (call, kept): call() evicts from src into dst."""
+    args, kept, keep = _evict_args(src, dst, budget, n_sinks, n_recent, kept, stream)
+    return PreparedCall(lib().glance_cache_evict, args, keep), kept

@@ -61,6 +61,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void attn_merge_kernel(AttnParams
 
   int ctx = p.ctx_lens[b];
   ctx = ctx < 0 ? 0 : (ctx > p.cap ? p.cap : ctx);
+  if (p.window) ctx = windowed_len(p, ctx);
   const int nsb = ctx > 0 ? (ctx + p.split_keys - 1) / p.split_keys : 1;
 
   const size_t base = ((size_t)b * p.hkv + g) * p.nsplit * p.rows_pad + r;
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(256) void attn_merge_pieces(AttnParams p) {
 // pieces: 20.0 us with 16, 18.8 with 24, 20.0 with 32; 37 rows of 64 dims,
 // about 10 pieces: 24.8 with 16, 25.3 with 24 and 32.
 static int merge_chunk(const AttnParams& p) {
-  const long tiles = ((long)p.cap + 63) / 64 + 1;
+  const long tiles = p.window ? (long)tile_map<64>(p, p.cap).n + 1 : ((long)p.cap + 63) / 64 + 1;
   long t = (tiles * p.batch + p.slots_per_g - 1) / p.slots_per_g;
   const long least = least_piece(p, (int)tiles);
   if (t < least) t = least;

@@ -51,6 +51,65 @@ __device__ __forceinline__ int clamp_ctx(int ctx, int cap) { return ctx < 0 ? 0 
 // tiles of a sequence: its context tiles, then the tile of new keys
 __device__ __forceinline__ int seq_tiles(int ctx) { return (ctx + 63) / 64 + 1; }
 
+// The context tiles of U keys that a windowed call reads: the `head` first ones,
+// which hold the sinks, then those from the first key that row 0 (the rows
+// after it see no earlier one) has in its window.  Tile j of the n read is tile
+// j, or j + skip past the sinks'.
+struct TileMap {
+  int head, skip, n;
+  int lo;  // first key of row 0's window
+  __host__ __device__ __forceinline__ int at(int j) const { return j < head ? j : j + skip; }
+};
+template <int U>
+__host__ __device__ __forceinline__ TileMap tile_map(const AttnParams& p, int ctx) {
+  TileMap m;
+  const int all = (ctx + U - 1) / U;
+  m.lo = ctx - p.window + 1;
+  if (m.lo < 0) m.lo = 0;
+  m.head = ((p.n_sinks < ctx ? p.n_sinks : ctx) + U - 1) / U;
+  int first = all;
+  if (m.lo < ctx) first = m.lo / U > m.head ? m.lo / U : m.head;
+  m.skip = first - m.head;
+  m.n = all - m.skip;
+  return m;
+}
+// Context keys that a windowed call of the fp32 kernel reads, in blocks of 16
+// (the keys of the blocks that are read, laid end to end).
+__host__ __device__ __forceinline__ int windowed_len(const AttnParams& p, int ctx) {
+  const TileMap m = tile_map<16>(p, ctx);
+  const int heads = 16 * m.head < ctx ? 16 * m.head : ctx;
+  return m.n > m.head ? ctx - 16 * m.skip : heads;
+}
+// Row r of a context tile from key0 on whose rows past `nvalid` do not exist,
+// or the nearest row that some new row sees: what lies outside the window is
+// not read, whatever it holds.
+__device__ __forceinline__ int seen_row(const TileMap& m, int n_sinks, int key0, int r, int nvalid) {
+  r = r < nvalid ? r : nvalid - 1;
+  const int key = key0 + r;
+  if (key >= n_sinks && key < m.lo) r = m.lo < key0 + nvalid ? m.lo - key0 : n_sinks - 1 - key0;
+  return r;
+}
+// bits 0 .. x - 1 of a 64-bit word
+__device__ __forceinline__ unsigned long long bits_below(int x) {
+  return x <= 0 ? 0ull : x >= 64 ? ~0ull : (1ull << x) - 1;
+}
+// The keys (bit k: key0 + k) that a row with `low` as the first key of its
+// window sees.
+__device__ __forceinline__ unsigned long long window_word(int n_sinks, int low, int key0) {
+  return bits_below(n_sinks - key0) | ~bits_below(low - key0);
+}
+// Lane i's ancestor word without the ancestors that lie outside node i's
+// window (all lanes active); `depth` is the lane's node's.
+__device__ __forceinline__ unsigned long long windowed_ancestors(const AttnParams& p, int ctx, unsigned long long anc,
+                                                                 int depth) {
+  if (p.window >= p.n) return anc;  // no node is that deep
+  for (int k = 0; k < p.n; ++k) {
+    const int dk = __builtin_amdgcn_readlane(depth, k);
+    if (depth - dk >= p.window && ctx + dk >= p.n_sinks) anc &= ~(1ull << k);
+  }
+  return anc;
+}
+
 struct Piece {
   int b;        // sequence
   int first;    // piece slot of the sequence's first piece (within the KV head)
@@ -99,7 +158,7 @@ __host__ __device__ __forceinline__ int least_piece(const AttnParams& p, int lon
 // sequence of 2048 keys took 15.1 us, with DPP reductions and the one-chunk
 // form 14.3 us.
 constexpr int kPlanCache = 4;
-template <bool ONE>
+template <bool ONE, bool WIN>
 __device__ __forceinline__ bool find_piece_in(const AttnParams& p, int ps, int lane, Piece& out) {
   constexpr int CACHE = ONE ? 1 : kPlanCache;
   int ctx_c[CACHE];
@@ -114,7 +173,7 @@ __device__ __forceinline__ bool find_piece_in(const AttnParams& p, int ps, int l
   };
   auto len_of = [&](int k) __attribute__((always_inline)) {
     const int ctx = ctx_of(k);
-    return ctx < 0 ? 0 : seq_tiles(ctx);
+    return ctx < 0 ? 0 : WIN ? tile_map<64>(p, ctx).n + 1 : seq_tiles(ctx);
   };
   const int chunks = ONE ? 1 : (p.batch + 63) / 64;
   int total = 0, longest = 0;
@@ -168,8 +227,9 @@ __device__ __forceinline__ bool find_piece_in(const AttnParams& p, int ps, int l
   }
   return false;
 }
+template <bool WIN = false>
 __device__ __forceinline__ bool find_piece(const AttnParams& p, int ps, int lane, Piece& out) {
-  return p.batch <= 64 ? find_piece_in<true>(p, ps, lane, out) : find_piece_in<false>(p, ps, lane, out);
+  return p.batch <= 64 ? find_piece_in<true, WIN>(p, ps, lane, out) : find_piece_in<false, WIN>(p, ps, lane, out);
 }
 
 // Ancestor words of a packed tree, anc[i] = {i} u anc[parent(i)], lane i's in

@@ -12,15 +12,16 @@
 
 #include <cfloat>
 
-#include "glance_internal.h"
+#include "glance_host.h"
 
 namespace {
-
 thread_local std::string g_last_error;
 thread_local hipEvent_t g_ev_start = nullptr;
 thread_local hipEvent_t g_ev_stop = nullptr;
+}  // namespace
 
-glance_status fail(glance_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace glance {
+
 glance_status fail(glance_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -31,9 +32,9 @@ glance_status fail(glance_status st, const char* fmt, ...) {
   return st;
 }
 
-glance_status ok() { return GLANCE_OK; }
+namespace {
 
-bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
+glance_status ok() { return GLANCE_OK; }
 
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -51,8 +52,9 @@ size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 //    one workgroup per compute unit (measured: two take 55 us instead of 48 at
 //    64 rows, 28/4 heads of 128, 4096 keys).  At most 4096 keys each, so that
 //    a ragged batch ends evenly.
-void plan_f32(const glance_attn_shape& s, int rows, int* rows_rg, int* split_keys) {
-  const long long keys = (long long)s.ctx_capacity + s.n_new;
+// A windowed call's context keys are those it reads at most (`ctx_keys`).
+void plan_f32(const glance_attn_shape& s, long long ctx_keys, int rows, int* rows_rg, int* split_keys) {
+  const long long keys = ctx_keys + s.n_new;
   const long long problems = (long long)s.batch * s.n_kv_heads;
   long long per;
   if (problems * ((rows + 15) / 16) * ((keys + 127) / 128) <= 256) {
@@ -67,15 +69,6 @@ void plan_f32(const glance_attn_shape& s, int rows, int* rows_rg, int* split_key
   *split_keys = (int)((per + 15) / 16 * 16);
 }
 
-// Attention workspace: [piece table][(max, sum) partials][O partials].
-struct Plan {
-  glance::AttnParams p;
-  size_t counter_bytes;  // the bf16 path's per-sequence piece table
-  size_t part_ml_bytes;
-  size_t part_o_bytes;
-  size_t total;
-};
-
 // A glance_dtype as the integer the caller stored: a C caller may store any
 // int in the field, and reading an out-of-range value as the C++ enum type
 // would be undefined, so the bits are copied out and compared as an int.
@@ -85,10 +78,14 @@ int dtype_bits(const glance_dtype& d) {
   return v;
 }
 
+}  // namespace
+
 bool dtype_ok(const glance_dtype& d) {
   const int v = dtype_bits(d);
   return v == GLANCE_F32 || v == GLANCE_BF16;
 }
+
+namespace {
 
 glance_status check_shape(const glance_attn_shape* s) {
   if (!s) return fail(GLANCE_ERR_INVALID_ARG, "shape is NULL");
@@ -115,10 +112,14 @@ glance_status check_shape(const glance_attn_shape* s) {
   return ok();
 }
 
-glance_status make_plan(const glance_attn_shape* s, Plan* out) {
+}  // namespace
+
+glance_status make_plan(const glance_attn_shape* s, int n_sinks, int window, Plan* out) {
   glance_status st = check_shape(s);
   if (st != GLANCE_OK) return st;
-  glance::AttnParams p = {};
+  AttnParams p = {};
+  p.n_sinks = n_sinks;
+  p.window = window;
   p.batch = s->batch;
   p.n = s->n_new;
   p.hq = s->n_q_heads;
@@ -149,10 +150,17 @@ glance_status make_plan(const glance_attn_shape* s, Plan* out) {
     pl.part_ml_bytes = round_up(wslots * p.rows_rg * sizeof(float2), 256);
     pl.part_o_bytes = round_up(wslots * p.rows_rg * p.d * sizeof(uint16_t), 256);  // fp16
   } else {
-    plan_f32(*s, p.rows, &p.rows_rg, &p.split_keys);
+    // context keys read at most: the sinks' blocks of 16, the window without
+    // its own row, and the rest of the block that the window begins in
+    long long keys = p.cap;
+    if (window) {
+      const long long most = ((long long)(n_sinks < p.cap ? n_sinks : p.cap) + 15) / 16 * 16 + window + 15LL;
+      if (most < keys) keys = most;
+    }
+    plan_f32(*s, keys, p.rows, &p.rows_rg, &p.split_keys);
     p.row_groups = (p.rows + p.rows_rg - 1) / p.rows_rg;
     p.rows_pad = p.row_groups * p.rows_rg;
-    p.nsplit = p.cap > 0 ? (p.cap + p.split_keys - 1) / p.split_keys : 1;
+    p.nsplit = keys > 0 ? (int)((keys + p.split_keys - 1) / p.split_keys) : 1;
     const size_t slots = (size_t)p.batch * p.hkv * p.nsplit * p.rows_pad;
     pl.counter_bytes = 0;
     pl.part_ml_bytes = round_up(slots * sizeof(float2), 256);
@@ -175,13 +183,10 @@ void take_events(hipEvent_t* a, hipEvent_t* b) {
   g_ev_start = g_ev_stop = nullptr;
 }
 
-glance_status attn_common(bool tree, const glance_attn_shape* s, const void* q, const void* k_ctx,
-                          const void* v_ctx, const void* k_new, const void* v_new,
-                          const int32_t* ctx_lens, const int32_t* parents, void* out, float* lse,
-                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  Plan pl;
-  glance_status st = make_plan(s, &pl);
-  if (st != GLANCE_OK) return st;
+glance_status bind_attn(const glance_attn_shape* s, const Plan& pl, bool tree, const void* q, const void* k_ctx,
+                        const void* v_ctx, const void* k_new, const void* v_new, const int32_t* ctx_lens,
+                        const int32_t* parents, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                        AttnParams* params) {
   struct {
     const void* ptr;
     const char* name;
@@ -206,7 +211,8 @@ glance_status attn_common(bool tree, const glance_attn_shape* s, const void* q, 
     return fail(GLANCE_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes,
                 pl.total);
 
-  glance::AttnParams p = pl.p;
+  AttnParams& p = *params;
+  p = pl.p;
   p.q = q;
   p.k_ctx = k_ctx;
   p.v_ctx = v_ctx;
@@ -220,15 +226,31 @@ glance_status attn_common(bool tree, const glance_attn_shape* s, const void* q, 
   p.part_o = reinterpret_cast<float*>(ws + pl.counter_bytes + pl.part_ml_bytes);
   p.out = out;
   p.lse = lse;
+  return ok();
+}
+
+namespace {
+
+glance_status attn_common(bool tree, const glance_attn_shape* s, const void* q, const void* k_ctx,
+                          const void* v_ctx, const void* k_new, const void* v_new,
+                          const int32_t* ctx_lens, const int32_t* parents, void* out, float* lse,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  Plan pl;
+  AttnParams p;
+  glance_status st = make_plan(s, 0, 0, &pl);
+  if (st == GLANCE_OK)
+    st = bind_attn(s, pl, tree, q, k_ctx, v_ctx, k_new, v_new, ctx_lens, parents, out, lse, workspace,
+                   workspace_bytes, &p);
+  if (st != GLANCE_OK) return st;
   hipEvent_t e0, e1;
   take_events(&e0, &e1);
   // the profiling events bracket the attention kernel (not the merge pass)
-  hipError_t e = s->dtype == GLANCE_BF16 ? glance::launch_attn_bf16(p, tree, stream, e0, e1)
-                                         : glance::launch_attn_f32(p, tree, stream, e0, e1);
+  hipError_t e = s->dtype == GLANCE_BF16 ? launch_attn_bf16(p, tree, stream, e0, e1)
+                                         : launch_attn_f32(p, tree, stream, e0, e1);
   if ((st = check_hip(e, "attention kernel launch")) != GLANCE_OK) return st;
   if (s->dtype == GLANCE_F32 && p.nsplit == 1) return ok();  // every workgroup wrote its rows' output
-  e = s->dtype == GLANCE_BF16 ? glance::launch_attn_merge_pieces(p, stream)
-                              : glance::launch_attn_merge(p, stream);
+  e = s->dtype == GLANCE_BF16 ? launch_attn_merge_pieces(p, stream)
+                              : launch_attn_merge(p, stream);
   return check_hip(e, "merge kernel launch");
 }
 
@@ -280,26 +302,26 @@ glance_status accept_plan(int32_t batch, int32_t n_nodes, int32_t vocab, AcceptP
   // workgroup per chunk of the argmax fits)
   out->ent_off = round_up((size_t)rows * chunks * sizeof(unsigned long long), 256);
   const long long room = (long long)((out->bytes - out->ent_off) / sizeof(float4)) / batch;
-  const long long steps = ((long long)vocab + glance::kEntropyStep - 1) / glance::kEntropyStep;
+  const long long steps = ((long long)vocab + kEntropyStep - 1) / kEntropyStep;
   const long long per_wg = (steps + room - 1) / room;
-  out->ent_len = (int)(per_wg * glance::kEntropyStep);
+  out->ent_len = (int)(per_wg * kEntropyStep);
   out->ent_chunks = (int)((steps + per_wg - 1) / per_wg);
   return ok();
 }
 
 struct TreePlan {
-  glance::TreeParams p;  // sizes and workspace offsets; pointers filled per call
+  TreeParams p;  // sizes and workspace offsets; pointers filled per call
   size_t off_stats, off_sketch, off_thr, off_cand, off_ccount, off_lq, off_tok, bytes;
 };
 
 glance_status tree_plan(int32_t batch, int32_t horizon, int32_t vocab, int32_t budget, TreePlan* out) {
   if (batch < 1) return fail(GLANCE_ERR_INVALID_ARG, "batch must be >= 1 (got %d)", batch);
   if (horizon < 1) return fail(GLANCE_ERR_INVALID_ARG, "horizon must be >= 1 (got %d)", horizon);
-  if (horizon > glance::kTreeMaxHorizon)
-    return fail(GLANCE_ERR_UNSUPPORTED, "horizon must be <= %d (got %d)", glance::kTreeMaxHorizon, horizon);
+  if (horizon > kTreeMaxHorizon)
+    return fail(GLANCE_ERR_UNSUPPORTED, "horizon must be <= %d (got %d)", kTreeMaxHorizon, horizon);
   if (budget < 1) return fail(GLANCE_ERR_INVALID_ARG, "budget must be >= 1 (got %d)", budget);
-  if (budget > glance::kTreeMaxBudget)
-    return fail(GLANCE_ERR_UNSUPPORTED, "budget must be <= %d (got %d)", glance::kTreeMaxBudget, budget);
+  if (budget > kTreeMaxBudget)
+    return fail(GLANCE_ERR_UNSUPPORTED, "budget must be <= %d (got %d)", kTreeMaxBudget, budget);
   if (vocab < 1 || vocab > (1 << 30)) return fail(GLANCE_ERR_INVALID_ARG, "vocab must be in 1..2^30");
   // the strings of length 1..horizon must number at least `budget`
   long long strings = 0, pw = 1;
@@ -313,17 +335,17 @@ glance_status tree_plan(int32_t batch, int32_t horizon, int32_t vocab, int32_t b
   const long long rows = (long long)batch * horizon;
   if (rows > 65535) return fail(GLANCE_ERR_UNSUPPORTED, "batch * horizon must be <= 65535");
   if (rows * (long long)vocab > (1LL << 40)) return fail(GLANCE_ERR_UNSUPPORTED, "draft logits too large");
-  glance::TreeParams p = {};
+  TreeParams p = {};
   p.batch = batch;
   p.horizon = horizon;
   p.vocab = vocab;
   p.budget = budget;
   p.k = budget < vocab ? budget : vocab;
-  p.slices = (vocab + glance::kTreeSlice - 1) / glance::kTreeSlice;
+  p.slices = (vocab + kTreeSlice - 1) / kTreeSlice;
   p.groups = 1;
   while ((long long)p.slices * p.groups < p.k && p.groups < 64) p.groups *= 2;
-  p.wgs_per_row = (p.slices + glance::kTreeScanWaves * glance::kTreeSlicesPerWave - 1) /
-                  (glance::kTreeScanWaves * glance::kTreeSlicesPerWave);
+  p.wgs_per_row = (p.slices + kTreeScanWaves * kTreeSlicesPerWave - 1) /
+                  (kTreeScanWaves * kTreeSlicesPerWave);
   TreePlan pl;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -334,7 +356,7 @@ glance_status tree_plan(int32_t batch, int32_t horizon, int32_t vocab, int32_t b
   pl.off_stats = take((size_t)rows * p.slices * sizeof(float2));
   pl.off_sketch = take((size_t)rows * p.slices * p.groups * sizeof(float));
   pl.off_thr = take((size_t)rows * p.slices * sizeof(float));
-  pl.off_cand = take((size_t)rows * p.slices * glance::kTreeSliceCap * sizeof(unsigned long long));
+  pl.off_cand = take((size_t)rows * p.slices * kTreeSliceCap * sizeof(unsigned long long));
   pl.off_ccount = take((size_t)rows * p.slices * sizeof(int32_t));
   pl.off_lq = take((size_t)rows * 64 * sizeof(float));
   pl.off_tok = take((size_t)rows * 64 * sizeof(int32_t));
@@ -345,6 +367,9 @@ glance_status tree_plan(int32_t batch, int32_t horizon, int32_t vocab, int32_t b
 }
 
 }  // namespace
+}  // namespace glance
+
+using namespace glance;
 
 extern "C" {
 
@@ -365,7 +390,7 @@ glance_status glance_tree_verify_attn(const glance_attn_shape* s, const void* q,
                      workspace_bytes, stream);
 }
 
-void bind_accept_workspace(glance::AcceptParams* p, const AcceptPlan& pl, void* workspace) {
+void bind_accept_workspace(AcceptParams* p, const AcceptPlan& pl, void* workspace) {
   p->part = static_cast<unsigned long long*>(workspace);
   p->ent_part = reinterpret_cast<float4*>(static_cast<char*>(workspace) + pl.ent_off);
 }
@@ -376,7 +401,7 @@ glance_status accept_setup(int32_t batch, int32_t n_nodes, int32_t vocab, glance
                            const void* logits, const int32_t* parents, const int32_t* tokens,
                            int32_t* rows_out, const char* rows_name, int32_t* accept_len,
                            int32_t* accept_path, int32_t path_stride, int32_t* next_root, void* workspace,
-                           size_t workspace_bytes, AcceptPlan* pl, glance::AcceptParams* p) {
+                           size_t workspace_bytes, AcceptPlan* pl, AcceptParams* p) {
   glance_status st = accept_plan(batch, n_nodes, vocab, pl);
   if (st != GLANCE_OK) return st;
   if (!dtype_ok(logits_dtype)) return fail(GLANCE_ERR_UNSUPPORTED, "logits dtype must be GLANCE_F32 or GLANCE_BF16");
@@ -399,7 +424,7 @@ glance_status accept_setup(int32_t batch, int32_t n_nodes, int32_t vocab, glance
   if (workspace_bytes < pl->bytes)
     return fail(GLANCE_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes,
                 pl->bytes);
-  *p = glance::AcceptParams{};
+  *p = AcceptParams{};
   p->logits = logits;
   p->parents = parents;
   p->tokens = tokens;
@@ -424,7 +449,7 @@ glance_status greedy_accept(int32_t batch, int32_t n_nodes, int32_t vocab, glanc
                             int32_t* next_root, float* root_entropy, void* workspace, size_t workspace_bytes,
                             hipStream_t stream) {
   AcceptPlan pl;
-  glance::AcceptParams p;
+  AcceptParams p;
   glance_status st = accept_setup(batch, n_nodes, vocab, logits_dtype, logits, parents, tokens, argmax_out,
                                   "argmax_out", accept_len, accept_path, path_stride, next_root, workspace,
                                   workspace_bytes, &pl, &p);
@@ -436,7 +461,7 @@ glance_status greedy_accept(int32_t batch, int32_t n_nodes, int32_t vocab, glanc
   p.chunk_len = pl.chunk_len;
   hipEvent_t e0, e1;
   take_events(&e0, &e1);
-  return check_hip(glance::launch_accept(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
+  return check_hip(launch_accept(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
                    "accept kernel launch");
 }
 }  // namespace
@@ -459,25 +484,25 @@ glance_status glance_greedy_accept_noalloc(int32_t batch, int32_t n_nodes, int32
   AcceptPlan pl;
   glance_status st = accept_plan(batch, n_nodes, vocab, &pl);
   if (st != GLANCE_OK) return st;
-  const size_t cap = glance::noalloc_scratch_bytes();
+  const size_t cap = noalloc_scratch_bytes();
   if (pl.bytes > cap)
     return fail(GLANCE_ERR_UNSUPPORTED,
                 "batch %d x n_nodes %d x vocab %d needs %zu bytes of scratch; the static buffer holds %zu",
                 batch, n_nodes, vocab, pl.bytes, cap);
   // every host check first, against an aligned placeholder of the right size
-  glance::AcceptParams p;
+  AcceptParams p;
   st = accept_setup(batch, n_nodes, vocab, logits_dtype, logits, parents, tokens, argmax_out, "argmax_out",
                     accept_len, accept_path, path_stride, next_root, reinterpret_cast<void*>(uintptr_t(256)),
                     pl.bytes, &pl, &p);
   if (st != GLANCE_OK) return st;
   void* ws = nullptr;
-  if ((st = check_hip(glance::noalloc_scratch(&ws), "scratch address lookup")) != GLANCE_OK) return st;
+  if ((st = check_hip(noalloc_scratch(&ws), "scratch address lookup")) != GLANCE_OK) return st;
   bind_accept_workspace(&p, pl, ws);
   p.chunks = pl.chunks;
   p.chunk_len = pl.chunk_len;
   hipEvent_t e0, e1;
   take_events(&e0, &e1);
-  return check_hip(glance::launch_accept(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
+  return check_hip(launch_accept(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
                    "accept kernel launch");
 }
 
@@ -500,7 +525,7 @@ glance_status glance_sample_accept(int32_t batch, int32_t n_nodes, int32_t vocab
                                    int32_t* next_root, void* workspace, size_t workspace_bytes,
                                    hipStream_t stream) {
   AcceptPlan pl;
-  glance::AcceptParams p;
+  AcceptParams p;
   glance_status st = accept_setup(batch, n_nodes, vocab, logits_dtype, logits, parents, tokens, draws_out,
                                   "draws_out", accept_len, accept_path, path_stride, next_root, workspace,
                                   workspace_bytes, &pl, &p);
@@ -520,7 +545,7 @@ glance_status glance_sample_accept(int32_t batch, int32_t n_nodes, int32_t vocab
   p.round_counter = round_counter;
   hipEvent_t e0, e1;
   take_events(&e0, &e1);
-  return check_hip(glance::launch_sample(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
+  return check_hip(launch_sample(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
                    "sample kernel launch");
 }
 
@@ -556,7 +581,7 @@ glance_status glance_build_tree(int32_t batch, int32_t horizon, int32_t vocab, i
   if (workspace_bytes < pl.bytes)
     return fail(GLANCE_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes,
                 pl.bytes);
-  glance::TreeParams p = pl.p;
+  TreeParams p = pl.p;
   char* ws = static_cast<char*>(workspace);
   p.logits = draft_logits;
   p.seq_stride = seq_stride;
@@ -573,7 +598,7 @@ glance_status glance_build_tree(int32_t batch, int32_t horizon, int32_t vocab, i
   p.ccount = reinterpret_cast<int32_t*>(ws + pl.off_ccount);
   hipEvent_t e0, e1;
   take_events(&e0, &e1);
-  return check_hip(glance::launch_tree(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
+  return check_hip(launch_tree(p, logits_dtype == GLANCE_BF16, stream, e0, e1),
                    "tree builder kernel launch");
 }
 
@@ -613,7 +638,7 @@ glance_status glance_commit_path(int32_t batch, int32_t n_nodes, int32_t n_kv_he
     if (reinterpret_cast<uintptr_t>(r.ptr) & (r.align - 1))
       return fail(GLANCE_ERR_INVALID_ARG, "%s is not %zu-byte aligned", r.name, r.align);
   }
-  glance::CommitParams p = {};
+  CommitParams p = {};
   p.k_new = k_new;
   p.v_new = v_new;
   p.accept_len = accept_len;
@@ -632,13 +657,13 @@ glance_status glance_commit_path(int32_t batch, int32_t n_nodes, int32_t n_kv_he
           aligned16(v_ctx);
   hipEvent_t e0, e1;
   take_events(&e0, &e1);
-  return check_hip(glance::launch_commit(p, stream, e0, e1), "commit kernel launch");
+  return check_hip(launch_commit(p, stream, e0, e1), "commit kernel launch");
 }
 
 size_t glance_attn_workspace_size(const glance_attn_shape* s, int is_verify) {
   (void)is_verify;  // the draft and the verify of one shape share a plan
   Plan pl;
-  if (make_plan(s, &pl) != GLANCE_OK) return 0;
+  if (make_plan(s, 0, 0, &pl) != GLANCE_OK) return 0;
   return pl.total;
 }
 
@@ -692,6 +717,6 @@ glance_status glance_set_kernel_events(void* start_event, void* stop_event) {
   return ok();
 }
 
-int32_t glance_version(void) { return 300; }
+int32_t glance_version(void) { return 400; }
 
 }  // extern "C"

@@ -43,7 +43,14 @@ struct AttnParams {
   int tiles_rg;     // 32-row tiles per row group (= computing waves, 1..7)
   int rows_rg;      // 32 * tiles_rg; fp32 kernel: rows of a row tile, 16 or 32
   int2* plan;       // [batch] (pieces, first piece slot) of each sequence, for the merge pass
+  // reads of a context cache in part or in 4 bits
+  int n_sinks;      // first context slots that every row sees
+  int window;       // positions a row sees up to its own, or kNoWindow; 0 where the kernels have no such limit
+  const unsigned char* k_scale;  // 4-bit cache: [batch][hkv][cap][d / 32] exponents; k_ctx, v_ctx then hold codes,
+  const unsigned char* v_scale;  // [batch][hkv][cap][d / 2] bytes
 };
+
+constexpr int kNoWindow = 0x7fffffff;
 
 // Values of a root row that a workgroup of the root entropy takes at a time.
 constexpr int kEntropyStep = 8192;
@@ -125,14 +132,69 @@ struct CommitParams {
   int vec;  // rows are 16-byte multiples and every pointer is 16-byte aligned
 };
 
+// A context cache as the kernels see it (glance_cache in glance.h).
+struct CacheView {
+  unsigned char *k, *v;              // rows of row_bytes
+  unsigned char *k_scale, *v_scale;  // 4-bit cache: rows of d / 32 exponents
+  int32_t* lens;
+  float* weights;
+  int cap;
+  int row_bytes;
+  bool kv4;
+};
+
+struct CacheParams {
+  CacheView src, dst;
+  int batch, hkv, d;
+  bool bf16;  // type of the dense side
+};
+
+// Commit of an accepted path into a 4-bit cache (dst); rows as in CommitParams.
+struct CommitKv4Params {
+  CacheView dst;
+  const void* k_new;
+  const void* v_new;
+  const int32_t* accept_len;
+  const int32_t* accept_path;
+  int batch, hkv, d, n, path_stride;
+  bool bf16;
+};
+
+struct WeighParams {
+  CacheView cache;
+  const void* q;      // [batch][n][hq][d]
+  const float* lse;   // [batch][n][hq]
+  const void* k_new;  // [batch][n][hkv][d], or null without a path
+  const int32_t* accept_len;
+  const int32_t* accept_path;  // or null: every row
+  float* out;                  // [batch][hkv][cap]
+  int batch, n, hq, hkv, group, d, path_stride;
+  int n_sinks, window;
+  float scale_log2, decay;
+};
+
+struct EvictParams {
+  CacheView src, dst;
+  int32_t* kept;  // [batch][hkv][budget]
+  int batch, hkv, d, budget, n_sinks, n_recent;
+};
+
 hipError_t launch_attn_bf16(const AttnParams& p, bool tree, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_attn_f32(const AttnParams& p, bool tree, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_attn_cache_bf16(const AttnParams& p, bool kv4, bool tree, hipStream_t s, hipEvent_t ev0,
+                                  hipEvent_t ev1);
+hipError_t launch_attn_cache_f32(const AttnParams& p, bool kv4, bool tree, hipStream_t s, hipEvent_t ev0,
+                                 hipEvent_t ev1);
 hipError_t launch_attn_merge(const AttnParams& p, hipStream_t s);
 hipError_t launch_attn_merge_pieces(const AttnParams& p, hipStream_t s);
 hipError_t launch_accept(const AcceptParams& p, bool bf16, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_sample(const AcceptParams& p, bool bf16, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_tree(const TreeParams& p, bool bf16, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
 hipError_t launch_commit(const CommitParams& p, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_cache_convert(const CacheParams& p, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_commit_kv4(const CommitKv4Params& p, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_weigh(const WeighParams& p, bool bf16, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
+hipError_t launch_evict(const EvictParams& p, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
 
 // The static per-GPU scratch of the allocation-free entry points: its size,
 // and the current device's copy (looked up once per device).
