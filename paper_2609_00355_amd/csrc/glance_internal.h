@@ -171,6 +171,7 @@ struct WeighParams {
   int batch, n, hq, hkv, group, d, path_stride;
   int n_sinks, window;
   float scale_log2, decay;
+  AttnParams plan;  // piece plan of the context tiles (set by the launcher)
 };
 
 struct EvictParams {
