@@ -6,21 +6,31 @@
 // NaN counts as larger than every number.  Two launches:
 //
 // 1. evict_select, one workgroup per (sequence, KV head): the least kept weight
-//    by radix selection on order-preserving keys (four passes of eight bits over
-//    the weights, counted in LDS), then the kept slots in order by a prefix sum.
+//    by radix selection on order-preserving keys, then the kept slots in order
+//    by prefix sums.  The first count takes 11 bits (sign, exponent and two of
+//    the fraction), which leaves few enough keys to go on with in LDS.  Bound
+//    by latency: three reads of the weights from L2 and about twenty barriers.
 // 2. evict_gather: the kept rows of K, V, scales and weights, 16 bytes a lane
 //    where rows are that wide.  Bound by memory.
 #include "glance_internal.h"
+
+#include "attn_plan.h"
 
 namespace glance {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kChunk = 4 * kSelectThreads;  // slots the workgroup reads with one load a lane
+constexpr int kChunks = 4;                  // chunks in flight
+constexpr int kBins = 2048;
+constexpr int kListed = 4096;               // keys held in LDS
 
 // Unsigned order of weights: -0 and +0 are equal, every NaN is the largest.
+// Never 0, which stands for a slot that is not up for selection.
 __device__ __forceinline__ unsigned order_key(float w) {
   unsigned u = __builtin_bit_cast(unsigned, w);
   if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
@@ -31,11 +41,13 @@ __device__ __forceinline__ unsigned order_key(float w) {
 __device__ __forceinline__ int clamp_len(int len, int cap) { return len < 0 ? 0 : (len > cap ? cap : len); }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
-  __shared__ unsigned s_hist[256];
-  __shared__ unsigned s_prefix, s_need;
-  __shared__ int s_count[2][kSelectWaves];
+  __shared__ unsigned s_hist[kBins];
+  __shared__ unsigned s_list[kListed];
+  __shared__ unsigned s_sum[kSelectWaves], s_found[3], s_n;
+  __shared__ int2 s_count[2][kSelectWaves];
   const int head = blockIdx.x, b = head / p.hkv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = clamp_len(p.src.lens[b], p.src.cap);
   int* kept = p.kept + (size_t)head * p.budget;
   if (len <= p.budget) {
@@ -44,74 +56,167 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   }
   const float* w = p.src.weights + (size_t)head * p.src.cap;
   const int lo = p.n_sinks, hi = len - p.n_recent;  // slots that have to earn their place
-  const unsigned take = (unsigned)(p.budget - p.n_sinks - p.n_recent);
-  // the take-th largest key: its bits from the top, eight at a time; `need` of
-  // the keys that agree with the bits found so far are still to be counted
-  unsigned prefix = 0, need = take;
-  if (take > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) s_hist[tid] = 0;
+  unsigned need = (unsigned)(p.budget - p.n_sinks - p.n_recent);
+
+  // the keys of slots j0 + kChunk c + 4 tid + i, 0 for those not up for selection
+  auto read = [&](int j0, unsigned (&k)[kChunks][4]) __attribute__((always_inline)) {
+    typedef f32x4 __attribute__((aligned(4))) loose;
+    f32x4 v[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      const int j = j0 + kChunk * c + 4 * tid;
+      v[c] = f32x4{};
+      if (len >= 4) v[c] = *reinterpret_cast<const loose*>(w + min(j, len - 4));
+    }
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      const int j = j0 + kChunk * c + 4 * tid;
+      if (j > len - 4) {  // the last slots, one by one
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[c][i] = w[min(j + i, len - 1)];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[c][i] = j + i >= lo && j + i < hi ? order_key(v[c][i]) : 0u;
+    }
+  };
+
+  // The need-th largest key, its bits from the top, 11, 11 and 10 at a time: a
+  // count of the keys by their next bits, among those that agree with the bits
+  // found so far.  Once these fit they are copied to LDS.
+  unsigned prefix = 0, equal = 0;
+  bool listed = false;
+  int n_list = 0;
+  if (need > 0) {
+    for (int level = 0; level < 3; ++level) {
+      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0;
+      const int bins = level == 2 ? 1024 : kBins;
+      const unsigned known = level == 0 ? 0u : ~0u << (level == 1 ? 21 : 10);  // bits found so far
+      for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
+      if (tid == 0) s_n = 0;
       __syncthreads();
-      for (int j = lo + tid; j < hi; j += kSelectThreads) {
-        const unsigned k = order_key(w[j]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(k >> shift) & 255u], 1u);
+      auto count = [&](unsigned k) __attribute__((always_inline)) {
+        if (k != 0 && (k & known) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
+      };
+      if (listed) {
+        for (int i = tid; i < n_list; i += kSelectThreads) count(s_list[i]);
+      } else {
+        for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
+          unsigned k[kChunks][4];
+          read(j0, k);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) count(k[c][i]);
+        }
       }
       __syncthreads();
-      if (wave == 0) {
-        // lane l holds bins 255 - 4 l .. 252 - 4 l: counts from the largest bin on
-        unsigned c[4], mine = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = s_hist[255 - 4 * lane - i];
-          mine += c[i];
-        }
-        unsigned incl = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-          const unsigned o = __shfl_up(incl, off);
-          if (lane >= off) incl += o;
-        }
-        unsigned before = incl - mine;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < need && need <= before + c[i]) {  // one lane, one bin
-            s_prefix = prefix | (unsigned)(255 - 4 * lane - i) << shift;
-            s_need = need - before;
-          }
-          before += c[i];
-        }
+      // the bin in which the count from the top reaches `need`: every wave sums
+      // its 128 bins, and the one with the crossing finds it
+      const unsigned hi_bin = s_hist[kBins - 1 - 128 * wave - 2 * lane], lo_bin = s_hist[kBins - 2 - 128 * wave - 2 * lane];
+      const unsigned incl = (unsigned)wave_incl_sum((int)(hi_bin + lo_bin));
+      if (lane == 63) s_sum[wave] = incl;
+      __syncthreads();
+      unsigned before = 0;
+      for (int x = 0; x < kSelectWaves; ++x) before += x < wave ? s_sum[x] : 0u;
+      const unsigned at_hi = before + incl - hi_bin - lo_bin, at_lo = at_hi + hi_bin;
+      const bool in_hi = at_hi < need && need <= at_lo, in_lo = at_lo < need && need <= at_lo + lo_bin;
+      if (in_hi || in_lo) {  // one lane of the workgroup
+        s_found[0] = (unsigned)(kBins - 1 - 128 * wave - 2 * lane - (in_lo ? 1 : 0));
+        s_found[1] = need - (in_lo ? at_lo : at_hi);
+        s_found[2] = in_lo ? lo_bin : hi_bin;
       }
       __syncthreads();
-      prefix = s_prefix;
-      need = s_need;
+      prefix |= s_found[0] << shift;
+      need = s_found[1];
+      equal = s_found[2];
+      if (!listed && level < 2 && equal <= kListed) {
+        const unsigned mask = ~0u << shift;
+        for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
+          unsigned k[kChunks][4];
+          read(j0, k);
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (k[c][i] != 0 && (k[c][i] & mask) == prefix) s_list[atomicAdd(&s_n, 1u)] = k[c][i];
+        }
+        n_list = (int)equal;
+        listed = true;
+        __syncthreads();
+      }
     }
   }
-  // kept slots in order: those above the least kept key and the first `need`
-  // that equal it; a chunk of slots at a time
-  int out = 0, ties = 0;
-  for (int j0 = 0; j0 < len; j0 += kSelectThreads) {
-    const int j = j0 + tid;
-    const bool mid = j >= lo && j < hi;
-    const unsigned k = mid && take > 0 ? order_key(w[j]) : 0;
-    const bool tie = mid && take > 0 && k == prefix;
-    const unsigned long long tb = __ballot(tie);
-    if (lane == 0) s_count[0][wave] = __popcll(tb);
+  // Kept slots in order: those above the least kept key and the first `need` of
+  // the `equal` ones that are it.  A slot's place is the number kept before it:
+  // counts of two chunks share a word (at most 4096 each).
+  int out = 0, ties = 0;  // kept, and equal ones, in the chunks before
+  int turn = 0;
+  // exclusive sums over the workgroup of each chunk's counts, and their totals
+  auto scan = [&](int2 mine, int2& total) __attribute__((always_inline)) {
+    const int2 incl = make_int2(wave_incl_sum(mine.x), wave_incl_sum(mine.y));
+    int2* slot = s_count[turn];
+    turn ^= 1;  // (a barrier lies between two uses of a buffer)
+    if (lane == 63) slot[wave] = incl;
     __syncthreads();
-    int tie_rank = ties + __popcll(tb & ((1ull << lane) - 1));
+    int2 at = make_int2(incl.x - mine.x, incl.y - mine.y);
+    total = make_int2(0, 0);
+#pragma unroll
     for (int x = 0; x < kSelectWaves; ++x) {
-      tie_rank += x < wave ? s_count[0][x] : 0;
-      ties += s_count[0][x];
+      const int2 o = slot[x];
+      at.x += x < wave ? o.x : 0;
+      at.y += x < wave ? o.y : 0;
+      total.x += o.x;
+      total.y += o.y;
     }
-    const bool keep = j < len && (!mid || (take > 0 && (k > prefix || (tie && tie_rank < (int)need))));
-    const unsigned long long kb = __ballot(keep);
-    if (lane == 0) s_count[1][wave] = __popcll(kb);
-    __syncthreads();
-    int at = out + __popcll(kb & ((1ull << lane) - 1));
-    for (int x = 0; x < kSelectWaves; ++x) {
-      at += x < wave ? s_count[1][x] : 0;
-      out += s_count[1][x];
+    return at;
+  };
+  auto half = [](int2 v, int c) __attribute__((always_inline)) { return ((c & 2 ? v.y : v.x) >> (c & 1 ? 16 : 0)) & 0xffff; };
+  auto add = [](int2& v, int c, int n) __attribute__((always_inline)) { (c & 2 ? v.y : v.x) += n << (c & 1 ? 16 : 0); };
+  const bool some = need < equal;  // not all of the equal ones are kept
+  const bool none = p.budget == p.n_sinks + p.n_recent;
+  for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
+    unsigned k[kChunks][4];
+    read(j0, k);
+    int2 total;
+    if (some) {
+      int2 mine = make_int2(0, 0);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add(mine, c, k[c][i] == prefix ? 1 : 0);
+      const int2 at = scan(mine, total);
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        int rank = ties + half(at, c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (k[c][i] == prefix && rank++ >= (int)need) k[c][i] = 1;  // below every key
+        ties += half(total, c);
+      }
     }
-    if (keep) kept[at] = j;
+    unsigned keep[kChunks];
+    int2 mine = make_int2(0, 0);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      const int j = j0 + kChunk * c + 4 * tid;
+      keep[c] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool mid = k[c][i] != 0;
+        keep[c] |= (mid ? !none && k[c][i] >= prefix : j + i < len) ? 1u << i : 0u;
+      }
+      add(mine, c, __popc(keep[c]));
+    }
+    const int2 at = scan(mine, total);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      const int j = j0 + kChunk * c + 4 * tid;
+      int place = out + half(at, c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (keep[c] >> i & 1u) kept[place++] = j + i;
+      out += half(total, c);
+    }
   }
 }
 
