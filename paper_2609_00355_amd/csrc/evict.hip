@@ -9,7 +9,7 @@
 //    by radix selection on order-preserving keys, then the kept slots in order
 //    by prefix sums.  The first count takes 11 bits (sign, exponent and two of
 //    the fraction), which leaves few enough keys to go on with in LDS.  Bound
-//    by latency: three reads of the weights from L2 and about twenty barriers.
+//    by latency: one read of the weights and about fifteen barriers.
 // 2. evict_gather: the kept rows of K, V, scales and weights, 16 bytes a lane
 //    where rows are that wide.  Bound by memory.
 #include "glance_internal.h"
@@ -27,7 +27,8 @@ constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kChunk = 4 * kSelectThreads;  // slots the workgroup reads with one load a lane
 constexpr int kChunks = 4;                  // chunks in flight
 constexpr int kBins = 2048;
-constexpr int kListed = 4096;               // keys held in LDS
+constexpr int kHeld = 32768;                // keys held in LDS: those of the first slots
+constexpr int kListed = 4096;               // ... and those still in question
 
 // Unsigned order of weights: -0 and +0 are equal, every NaN is the largest.
 // Never 0, which stands for a slot that is not up for selection.
@@ -41,6 +42,7 @@ __device__ __forceinline__ unsigned order_key(float w) {
 __device__ __forceinline__ int clamp_len(int len, int cap) { return len < 0 ? 0 : (len > cap ? cap : len); }
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
+  __shared__ u32x4 s_keys[kHeld / 4];
   __shared__ unsigned s_hist[kBins];
   __shared__ unsigned s_list[kListed];
   __shared__ unsigned s_sum[kSelectWaves], s_found[3], s_n;
@@ -58,8 +60,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   const int lo = p.n_sinks, hi = len - p.n_recent;  // slots that have to earn their place
   unsigned need = (unsigned)(p.budget - p.n_sinks - p.n_recent);
 
-  // the keys of slots j0 + kChunk c + 4 tid + i, 0 for those not up for selection
-  auto read = [&](int j0, unsigned (&k)[kChunks][4]) __attribute__((always_inline)) {
+  // The keys of slots j0 + kChunk c + 4 tid + i, 0 for those not up for
+  // selection.  A thread's slots are its own in every pass, so it finds its
+  // keys in LDS without a barrier; only longer sequences' are read again.
+  auto fetch = [&](int j0, u32x4 (&k)[kChunks]) __attribute__((always_inline)) {
     typedef f32x4 __attribute__((aligned(4))) loose;
     f32x4 v[kChunks];
 #pragma unroll
@@ -77,12 +81,19 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) k[c][i] = j + i >= lo && j + i < hi ? order_key(v[c][i]) : 0u;
+      if (j0 < kHeld) s_keys[j / 4] = k[c];
     }
   };
+  auto read = [&](int j0, u32x4 (&k)[kChunks]) __attribute__((always_inline)) {
+    if (j0 >= kHeld) return fetch(j0, k);
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) k[c] = s_keys[(j0 + kChunk * c) / 4 + tid];
+  };
+  static_assert(kHeld % (kChunks * kChunk) == 0, "a read is held in whole or not at all");
 
   // The need-th largest key, its bits from the top, 11, 11 and 10 at a time: a
   // count of the keys by their next bits, among those that agree with the bits
-  // found so far.  Once these fit they are copied to LDS.
+  // found so far.  Once these fit they are copied into a list of their own.
   unsigned prefix = 0, equal = 0;
   bool listed = false;
   int n_list = 0;
@@ -101,8 +112,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
         for (int i = tid; i < n_list; i += kSelectThreads) count(s_list[i]);
       } else {
         for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
-          unsigned k[kChunks][4];
-          read(j0, k);
+          u32x4 k[kChunks];
+          if (level == 0) fetch(j0, k);
+          else read(j0, k);
 #pragma unroll
           for (int c = 0; c < kChunks; ++c)
 #pragma unroll
@@ -132,7 +144,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
       if (!listed && level < 2 && equal <= kListed) {
         const unsigned mask = ~0u << shift;
         for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
-          unsigned k[kChunks][4];
+          u32x4 k[kChunks];
           read(j0, k);
 #pragma unroll
           for (int c = 0; c < kChunks; ++c)
@@ -175,8 +187,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   const bool some = need < equal;  // not all of the equal ones are kept
   const bool none = p.budget == p.n_sinks + p.n_recent;
   for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
-    unsigned k[kChunks][4];
-    read(j0, k);
+    u32x4 k[kChunks];
+    if (none) fetch(j0, k);  // nothing was read before
+    else read(j0, k);
     int2 total;
     if (some) {
       int2 mine = make_int2(0, 0);
