@@ -30,16 +30,26 @@ constexpr int kBins = 2048;
 constexpr int kHeld = 32768;                // keys held in LDS: those of the first slots
 constexpr int kListed = 4096;               // ... and those still in question
 
-// Unsigned order of weights: -0 and +0 are equal, every NaN is the largest.
-// Never 0, which stands for a slot that is not up for selection.
+// Unsigned order of weights: -0 and +0 are equal, every NaN is the largest.  No
+// key is 0, which stands for a slot that is not up for selection.
 __device__ __forceinline__ unsigned order_key(float w) {
-  unsigned u = __builtin_bit_cast(unsigned, w);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-  if (u == 0x80000000u) u = 0;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const int u = __builtin_bit_cast(int, w + 0.f);  // -0 becomes +0
+  const unsigned k = (unsigned)(u ^ (u >> 31 | (int)0x80000000));
+  return w != w ? 0xffffffffu : k;
 }
 
 __device__ __forceinline__ int clamp_len(int len, int cap) { return len < 0 ? 0 : (len > cap ? cap : len); }
+
+// Inclusive prefix sum within each row of 16 lanes, all lanes active: with a
+// wave's count in lane `wave` of every row, what the waves before it counted.
+__device__ __forceinline__ int row_incl_sum(int v) {
+  v += plan_dpp<0x111, 0xf, 0>(v);  // row_shr:1
+  v += plan_dpp<0x112, 0xf, 0>(v);  // row_shr:2
+  v += plan_dpp<0x114, 0xf, 0>(v);  // row_shr:4
+  v += plan_dpp<0x118, 0xf, 0>(v);  // row_shr:8
+  return v;
+}
+static_assert(kSelectWaves == 16, "a row of lanes holds the waves' counts");
 
 __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   __shared__ u32x4 s_keys[kHeld / 4];
@@ -80,7 +90,12 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
         for (int i = 0; i < 4; ++i) v[c][i] = w[min(j + i, len - 1)];
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) k[c][i] = j + i >= lo && j + i < hi ? order_key(v[c][i]) : 0u;
+      for (int i = 0; i < 4; ++i) k[c][i] = order_key(v[c][i]);
+      const int first = j0 + kChunk * c;
+      if (first < lo || first + kChunk > hi) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[c][i] = j + i >= lo && j + i < hi ? k[c][i] : 0u;
+      }
       if (j0 < kHeld) s_keys[j / 4] = k[c];
     }
   };
@@ -106,19 +121,27 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
       if (tid == 0) s_n = 0;
       __syncthreads();
       auto count = [&](unsigned k) __attribute__((always_inline)) {
-        if (k != 0 && (k & known) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
+        if ((k & known) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
       };
       if (listed) {
         for (int i = tid; i < n_list; i += kSelectThreads) count(s_list[i]);
       } else {
         for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
           u32x4 k[kChunks];
-          if (level == 0) fetch(j0, k);
-          else read(j0, k);
+          if (level == 0) {
+            fetch(j0, k);
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c)
+            for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) count(k[c][i]);
+              for (int i = 0; i < 4; ++i)
+                if (k[c][i] != 0) atomicAdd(&s_hist[k[c][i] >> 21], 1u);
+          } else {
+            read(j0, k);
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) count(k[c][i]);
+          }
         }
       }
       __syncthreads();
@@ -128,8 +151,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
       const unsigned incl = (unsigned)wave_incl_sum((int)(hi_bin + lo_bin));
       if (lane == 63) s_sum[wave] = incl;
       __syncthreads();
-      unsigned before = 0;
-      for (int x = 0; x < kSelectWaves; ++x) before += x < wave ? s_sum[x] : 0u;
+      const int sum = (int)s_sum[lane & 15], sums = row_incl_sum(sum);
+      const unsigned before = (unsigned)__builtin_amdgcn_readlane(sums - sum, wave);
       const unsigned at_hi = before + incl - hi_bin - lo_bin, at_lo = at_hi + hi_bin;
       const bool in_hi = at_hi < need && need <= at_lo, in_lo = at_lo < need && need <= at_lo + lo_bin;
       if (in_hi || in_lo) {  // one lane of the workgroup
@@ -150,7 +173,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
           for (int c = 0; c < kChunks; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (k[c][i] != 0 && (k[c][i] & mask) == prefix) s_list[atomicAdd(&s_n, 1u)] = k[c][i];
+              if ((k[c][i] & mask) == prefix) s_list[atomicAdd(&s_n, 1u)] = k[c][i];
         }
         n_list = (int)equal;
         listed = true;
@@ -170,17 +193,10 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
     turn ^= 1;  // (a barrier lies between two uses of a buffer)
     if (lane == 63) slot[wave] = incl;
     __syncthreads();
-    int2 at = make_int2(incl.x - mine.x, incl.y - mine.y);
-    total = make_int2(0, 0);
-#pragma unroll
-    for (int x = 0; x < kSelectWaves; ++x) {
-      const int2 o = slot[x];
-      at.x += x < wave ? o.x : 0;
-      at.y += x < wave ? o.y : 0;
-      total.x += o.x;
-      total.y += o.y;
-    }
-    return at;
+    const int2 o = slot[lane & 15], sums = make_int2(row_incl_sum(o.x), row_incl_sum(o.y));
+    total = make_int2(__builtin_amdgcn_readlane(sums.x, 15), __builtin_amdgcn_readlane(sums.y, 15));
+    return make_int2(incl.x - mine.x + __builtin_amdgcn_readlane(sums.x - o.x, wave),
+                     incl.y - mine.y + __builtin_amdgcn_readlane(sums.y - o.y, wave));
   };
   auto half = [](int2 v, int c) __attribute__((always_inline)) { return ((c & 2 ? v.y : v.x) >> (c & 1 ? 16 : 0)) & 0xffff; };
   auto add = [](int2& v, int c, int n) __attribute__((always_inline)) { (c & 2 ? v.y : v.x) += n << (c & 1 ? 16 : 0); };

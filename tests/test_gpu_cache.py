@@ -351,6 +351,24 @@ def test_evict(fmt, dtype, d, budget, n_sinks, n_recent):
                 assert (t[b, g, len(slots):] == 7).all()
 
 
+def test_evict_from_long_contexts():
+    """More slots than the selection holds at a time, few and many equal weights, more kept slots than it stages."""
+    lens, budget = [70001, 32769, 33000], 9000
+    g = torch.Generator().manual_seed(2)
+    w = torch.rand(3, 1, 70001, generator=g)
+    w[1] = (w[1] * 4).floor() / 4       # four values: thousands of ties
+    w[2, 0, ::2] = 0.5
+    k = torch.arange(70001, dtype=torch.float32).reshape(1, 1, -1, 1).expand(3, 1, -1, 64).contiguous().cuda()
+    src = G.ContextCache(k, k.clone(), torch.tensor(lens, dtype=torch.int32).cuda(), weights=w.cuda())
+    to = G.new_cache(3, 1, budget, 64, dtype=torch.float32, weights=True)
+    kept = G.glance_cache_evict(src, to, budget, 10, 700)
+    torch.cuda.synchronize()
+    want = OC.evict(lens, w.numpy(), budget, 10, 700)
+    for b in range(3):
+        assert kept[b, 0].cpu().tolist() == want[b][0]
+        assert to.v[b, 0, :, 63].cpu().tolist() == [float(x) for x in want[b][0]]
+
+
 def test_evict_with_shared_lengths():
     c = Case("bf16", "dense", 64, 1, 2, 2, [200, 30], seed=1, weights=True)
     to = G.new_cache(2, 2, 64, 64, weights=True)
