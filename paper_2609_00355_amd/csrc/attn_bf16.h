@@ -134,7 +134,7 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // with KV4; kNoWindow there is the whole context).
 template <int D, bool TREE, bool WIDE, bool KV4 = false, bool WIN = KV4>
 __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
-  constexpr bool STAGED = KV4 || (WIDE && D == 64);  // loads by way of registers (see the ring rule)
+  constexpr bool STAGED = WIDE && D == 64 && !KV4;  // loads by way of registers (see the ring rule)
   using G_ = Geo<D>;
   constexpr int RB = G_::RB, CH = G_::CH, TB = G_::TB, KS = G_::KS, DB = G_::DB;
   constexpr int RPL = G_::RPL, NB = G_::NB, OV = G_::OV;
@@ -184,16 +184,18 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   const char* kn = static_cast<const char*>(p.k_new);
   const char* vn = static_cast<const char*>(p.v_new);
   // This wave's loads of a K (or V) tile: r = first + stride i, i < kLoads.
-  constexpr int kLoads = WIDE ? NB / 8 : NB / 4;
-  constexpr int stride = WIDE ? 8 : 4;
-  const int first = WIDE ? wave : wave - 4;
-  const bool loads = WIDE || wave >= 4;
+  // (A 4-bit cache's loads are a quarter, and go to registers: with five to seven
+  // computing waves wave 7, which has no rows, brings all of them.)
+  constexpr int stride = KV4 ? (WIDE ? 1 : 4) : WIDE ? 8 : 4;
+  constexpr int kLoads = NB / stride;
+  const int first = WIDE && !KV4 ? wave : wave - (8 - stride);
+  const bool loads = first >= 0;
   // Load r (0 <= r < NB) of a tile fills LDS rows r RPL .. r RPL + RPL - 1;
   // lane i writes row r RPL + i / CH, chunk slot i % CH, which holds the
   // row's chunk slot ^ swz(row).  The lane's row and its byte offset within
   // a full context tile (row stride RB) are computed once.
   constexpr int kStep = stride * RPL;  // rows between a wave's loads, a multiple of 16: the same chunk order
-  static_assert(kStep % 16 == 0, "swz has period 16");
+  static_assert(KV4 || kStep % 16 == 0, "swz has period 16");
   const int lrow = first * RPL + lane / CH;
   const unsigned lchunk = (unsigned)(((lane % CH) ^ swz<D>(lrow)) * 16);
   auto issue = [&](int t, bool v_side) __attribute__((always_inline)) {
@@ -227,7 +229,8 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     for (int i = 0; i < kLoads; ++i) {
       const int src = WIN && !KV4 && j < ct ? seen_row(tm, p.n_sinks, key0, lrow + i * kStep, nvalid)
                                             : min(lrow + i * kStep, nvalid - 1);
-      dma16(base, (unsigned)src * rstride + lchunk, lds + stride * i * 1024);
+      const unsigned chunk = kStep % 16 == 0 ? lchunk : (unsigned)(((lane % CH) ^ swz<D>(lrow + i * kStep)) * 16);
+      dma16(base, (unsigned)src * rstride + chunk, lds + stride * i * 1024);
     }
   };
   // Ring rule.  Tile t is read by the computing waves' matrix phases: K(t) in
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   };
   auto ring_wait = [&](int t) __attribute__((always_inline)) {
     if (t + 2 >= n_tiles) wait_vmcnt<0>();
-    else wait_vmcnt<4 * kLoads>();
+    else wait_vmcnt<KV4 ? 0 : 4 * kLoads>();
   };
 
   // Staged (64-dim heads): the prologue brings K(0), K(1) and V(0) by DMA and
@@ -307,7 +310,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   // they are older than the first set, whose store waits for it before barrier 1)
   auto stage_wait0 = [&]() __attribute__((always_inline)) {
     if (n_tiles == 1) wait_vmcnt<0>();
-    else wait_vmcnt<6 * kLoads>();
+    else wait_vmcnt<KV4 ? 0 : 6 * kLoads>();
   };
   auto stage_step = [&](int t, auto P_) __attribute__((always_inline)) {
     constexpr int P = decltype(P_)::value & 1;  // t's parity
@@ -317,93 +320,100 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     stage_load(t + 3, true, stV[P]);
   };
 
-  // 4-bit cache: the same schedule, and what a wave stores is the bf16 values of
-  // the codes it loaded (exact: three significant bits times a power of two),
-  // so the matrix phases are the dense cache's.  A lane's share of a tile is
-  // kLoads chunks of one row, 4 kLoads bytes of codes under one scale.  The
-  // tile of new keys, which is dense, comes by DMA: K at step tn - 2, V at step
+  // 4-bit cache: the schedule of the staged form, by the loading waves alone
+  // (one, or four where at most four compute), and what they store is the bf16
+  // values of the codes they loaded (exact: three significant bits times a power
+  // of two), so the matrix phases are the dense cache's.  A lane has one row of
+  // the tile, CPL chunks of it; rows side by side are stored without bank
+  // conflicts.  One wave converts a tile (128 conversions and 32 stores with 128
+  // dims) while its neighbour on the SIMD, alone there, computes; shared by all
+  // waves, that work took 50 vector instructions a tile from each.
+  // The tile of new keys, which is dense, comes by DMA: K at step tn - 2, V at step
   // tn - 1 (or in the prologue) into the stages that the codes would take, whose
   // stores go one stage further instead (K(t - 1)'s or V(t - 2)'s, free since
   // barrier t); every loading wave waits for it before barrier tn.
+  constexpr int CPL = CH / stride;  // chunks of a lane, 4 bytes of codes each
+  constexpr int SPL = CPL > 4 ? CPL / 4 : 1;  // scales of a lane
   struct Codes {
-    unsigned c[kLoads], scale;
+    unsigned c[CPL], scale;
   };
-  constexpr int kParts = CH / kLoads;  // lanes a row
-  const int urow = (first * 64 + lane) / kParts, upart = (first * 64 + lane) % kParts;
   const int tn = KV4 && has_new ? n_tiles - 1 : -1;
   const int n_ctx = n_tiles - (has_new ? 1 : 0);  // context tiles of the piece
+  const size_t head_row = ((size_t)b * p.hkv + g) * p.cap;
+  const unsigned lcode = (unsigned)(first * CPL * 4), lscale = (unsigned)(first * CPL / 4);
   auto codes_load = [&](int t, bool v_side, Codes& r) __attribute__((always_inline)) {
     const int key0 = key_of(tb + min(t, max(n_ctx - 1, 0)));
-    const size_t at = ((size_t)b * p.hkv + g) * p.cap + (size_t)key0;
-    const char* base = (v_side ? vc : kc) + at * (D / 2);
-    const char* sbase = reinterpret_cast<const char*>(v_side ? p.v_scale : p.k_scale) + at * (D / 32);
-    int src = seen_row(tm, p.n_sinks, key0, urow, min(64, ctx - key0));
+    const char* base = (v_side ? vc : kc) + (head_row + key0) * (D / 2);
+    const char* sbase = reinterpret_cast<const char*>(v_side ? p.v_scale : p.k_scale) + (head_row + key0) * (D / 32);
+    unsigned src = (unsigned)seen_row(tm, p.n_sinks, key0, lane, min(64, ctx - key0));
     if (n_ctx == 0) {  // nothing of the cache is read: any valid address
       base = sbase = kn;
       src = 0;
     }
-    const char* a = base + (unsigned)src * (D / 2) + upart * (4 * kLoads);
-    if constexpr (kLoads == 4) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(a);
+    const unsigned at = src * (D / 2) + lcode, sat = src * (D / 32) + lscale;
+    if constexpr (CPL >= 4) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r.c[i] = w[i];
-    } else if constexpr (kLoads == 2) {
-      const uint2 w = *reinterpret_cast<const uint2*>(a);
+      for (int i = 0; i < CPL; i += 4) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(base + (at + 4 * i));
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r.c[i + x] = w[x];
+      }
+    } else {
+      const uint2 w = *reinterpret_cast<const uint2*>(base + at);
       r.c[0] = w.x;
       r.c[1] = w.y;
-    } else {
-      r.c[0] = *reinterpret_cast<const unsigned*>(a);
     }
-    r.scale = *reinterpret_cast<const unsigned char*>(sbase + (unsigned)src * (D / 32) + upart * kLoads / 4);
+    if constexpr (SPL == 4) r.scale = *reinterpret_cast<const unsigned*>(sbase + sat);
+    else if constexpr (SPL == 2) r.scale = *reinterpret_cast<const unsigned short*>(sbase + sat);
+    else r.scale = *reinterpret_cast<const unsigned char*>(sbase + sat);
   };
   auto codes_store = [&](int t, bool v_side, const Codes& r) __attribute__((always_inline)) {
     const int stage = (t + (t == tn ? 1 : 0)) % kStages;
-    lds_char* dst = (lds_char*)(v_side ? sV : sK) + stage * TB + urow * RB;
-    const float scale = __builtin_bit_cast(float, r.scale << 23);
+    lds_char* dst = (lds_char*)(v_side ? sV : sK) + stage * TB + lane * RB;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
+    for (int i = 0; i < CPL; ++i) {
+      const float scale = __builtin_bit_cast(float, (r.scale >> (8 * (i / 4)) & 255u) << 23);
       const u32x4 w = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], scale, 0)),
                        __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], scale, 1)),
                        __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], scale, 2)),
                        __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.c[i], scale, 3))};
-      *(lds_u32x4*)(dst + (((upart * kLoads + i) ^ swz<D>(urow)) * 16)) = w;
+      *(lds_u32x4*)(dst + (((first * CPL + i) ^ swz<D>(lane)) * 16)) = w;
     }
   };
-  Codes cK[2], cV[2];
-  auto codes_prologue = [&]() __attribute__((always_inline)) {
-    Codes k0, k1, v0;
-    codes_load(0, false, k0);
-    codes_load(1, false, k1);
-    codes_load(0, true, v0);
-    codes_load(2, false, cK[0]);
-    codes_load(1, true, cV[0]);
-    codes_load(3, false, cK[1]);
-    codes_load(2, true, cV[1]);
-    if (tn == 0 || tn == 1) issue(tn, false);
-    if (tn == 0) issue(tn, true);
-    codes_store(0, false, k0);
-    codes_store(1, false, k1);
-    codes_store(0, true, v0);
-  };
-  auto codes_step = [&](int t, auto P_) __attribute__((always_inline)) {
-    constexpr int P = decltype(P_)::value & 1;
-    codes_store(t + 2, false, cK[P]);
-    codes_store(t + 1, true, cV[P]);
-    codes_load(t + 4, false, cK[P]);
-    codes_load(t + 3, true, cV[P]);
-    if (t + 2 == tn) issue(tn, false);
-    if (t + 1 == tn) issue(tn, true);
-  };
-  auto codes_wait = [&](int t) __attribute__((always_inline)) {
-    if (t == tn) wait_vmcnt<0>();
-  };
-  auto reg_prologue = [&]() __attribute__((always_inline)) {
-    if constexpr (KV4) codes_prologue();
-    else stage_prologue();
-  };
-  auto reg_step = [&](int t, auto P_) __attribute__((always_inline)) {
-    if constexpr (KV4) codes_step(t, P_);
-    else stage_step(t, P_);
+  auto codes_wave = [&]() __attribute__((always_inline)) {
+    Codes cK[2], cV[2];
+    {
+      Codes k0, k1, v0;
+      codes_load(0, false, k0);
+      codes_load(1, false, k1);
+      codes_load(0, true, v0);
+      codes_load(2, false, cK[0]);
+      codes_load(1, true, cV[0]);
+      codes_load(3, false, cK[1]);
+      codes_load(2, true, cV[1]);
+      if (tn == 0 || tn == 1) issue(tn, false);
+      if (tn == 0) issue(tn, true);
+      codes_store(0, false, k0);
+      codes_store(1, false, k1);
+      codes_store(0, true, v0);
+    }
+    auto step = [&](int t, auto P_) __attribute__((always_inline)) {
+      constexpr int P = decltype(P_)::value;
+      if (t == tn) wait_vmcnt<0>();
+      lds_barrier();
+      codes_store(t + 2, false, cK[P]);
+      codes_store(t + 1, true, cV[P]);
+      codes_load(t + 4, false, cK[P]);
+      codes_load(t + 3, true, cV[P]);
+      if (t + 2 == tn) issue(tn, false);
+      if (t + 1 == tn) issue(tn, true);
+    };
+    for (int t = 0;;) {
+      step(t, std::integral_constant<int, 0>{});
+      if (++t >= n_tiles) break;
+      step(t, std::integral_constant<int, 1>{});
+      if (++t >= n_tiles) break;
+    }
   };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
@@ -413,22 +423,24 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   if (wave >= p.tiles_rg) {
     // a wave without rows: streams its share of the tiles and keeps the
     // barrier count
-    if (STAGED && loads) {
-      reg_prologue();
-      if (!KV4) stage_wait0();
+    if (STAGED) {
+      stage_prologue();
+      stage_wait0();
       for (int t = 0;;) {
-        if (KV4) codes_wait(t);
         lds_barrier();
-        reg_step(t, I0{});
+        stage_step(t, I0{});
         if (++t >= n_tiles) break;
-        if (KV4) codes_wait(t);
         lds_barrier();
-        reg_step(t, I1{});
+        stage_step(t, I1{});
         if (++t >= n_tiles) break;
       }
       return;
     }
-    const bool ring = !STAGED && loads;
+    if (KV4 && loads) {
+      codes_wave();
+      return;
+    }
+    const bool ring = loads && !KV4;
     if (ring) ring_prologue();
     for (int t = 0; t < n_tiles; ++t) {
       if (ring) ring_wait(t);
@@ -452,7 +464,8 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   // parents; staged loads follow them.  The compiler's waits for the query
   // count the loads it sees, not the DMA ones, so they also wait for the tiles
   // issued by DMA before it.
-  if (WIDE && !STAGED) ring_prologue();
+  constexpr bool RING = WIDE && !STAGED && !KV4;  // the computing waves take part in the ring
+  if (RING) ring_prologue();
   bf16x8 qf[KS];
   {
     const __bf16* qp = static_cast<const __bf16*>(p.q) + out_row * D + 8 * h;
@@ -462,7 +475,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   const bool tree_words = TREE && (has_new || WIN) && wave == 0;
   int par = -1;
   if (tree_words && lane < p.n) par = p.parents[(size_t)b * p.n + lane];
-  if (STAGED && WIDE) reg_prologue();
+  if (STAGED) stage_prologue();
   if (tree_words) {
     unsigned long long anc = ancestor_word(par, lane);
     if (WIN) {
@@ -647,8 +660,8 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
                                                         O[db], 0, 0, 0);
       }
       if (idx == NS / 2 && ti >= 0) {
-        if (STAGED && WIDE) reg_step(ti, SK_);
-        else if (!STAGED && WIDE) ring_issue(ti);
+        if (STAGED) stage_step(ti, SK_);
+        else if (RING) ring_issue(ti);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -678,21 +691,19 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   // and t + 1, and X_t reads only K(t) and V(t - 1).)
   using YES = std::true_type;
   using NO = std::false_type;
-  if (KV4 && WIDE) codes_wait(0);
-  else if (STAGED && WIDE) stage_wait0();
-  else if (WIDE) ring_wait(0);
+  if (STAGED) stage_wait0();
+  else if (RING) ring_wait(0);
   lds_barrier();  // barrier 0: K(0) has landed, the ancestor words are written
-  if (WIDE && !STAGED) ring_issue(0);
+  if (RING) ring_issue(0);
   xphase(I0{}, YES{}, NO{}, STAGED ? 0 : -1);
   auto step = [&](int t, auto SK_) __attribute__((always_inline)) {
     yphase(t - 1);
-    if (WIDE && !STAGED) ring_wait(t);
-    if (KV4 && WIDE) codes_wait(t);
+    if (RING) ring_wait(t);
     lds_barrier();  // barrier t: K(t) and V(t - 1) have landed, and X_{t-1} has ended everywhere
     // DMA by all waves: waves 0-3 issue right away, waves 4-6 halfway through
     // X_t, so that of the two computing waves sharing a SIMD one computes while
     // the other waits for the memory pipeline to take its loads
-    if (WIDE && !STAGED && wave < 4) ring_issue(t);
+    if (RING && wave < 4) ring_issue(t);
     xphase(SK_, YES{}, YES{}, STAGED || wave >= 4 ? t : -1);
   };
   int t = 1;
