@@ -9,11 +9,13 @@
 // no second pass, no atomics, the same bits every time.
 //
 // Work.  The context tiles of 64 keys that some row sees are cut into pieces of
-// equal size by the attention's plan (attn_plan.h), a workgroup each, whose waves
-// take its tiles in turn; slots that no row sees only fade, and the pieces of
-// their sequence share them.  The queries of up to kRows rows are staged in LDS
-// once a workgroup (more rows: in turn, the sums added up in the output), a
-// tile's keys are loaded into registers while the tile before is computed.
+// equal size by the attention's plan (attn_plan.h), a workgroup each, about one a
+// compute unit; its waves take the piece's tiles as they become free (a wave
+// that shares its SIMD with an older one gets two thirds of its turns).  Slots
+// that no row sees only fade, and the pieces of their sequence share them.  The
+// queries of up to kRows rows are staged in LDS once a workgroup (more rows: in
+// turn, the sums added up in the output), a tile's keys are loaded into registers
+// while the tile before is computed.
 //
 // S[row][key] = Q . K^T with the rows as matrix operand A: a lane's results are
 // 16 rows of one key, so the sums over rows are sums over a lane's registers
@@ -34,7 +36,7 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 
-constexpr int kWeighWaves = 4;
+constexpr int kWeighWaves = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // A lane's half of one row (a key or a query) as matrix operands: bf16 D / 16
@@ -49,9 +51,13 @@ struct Operand {
   static constexpr int N = D / (2 * W);                  // parts of a lane
   Part x[N];
   static __device__ __forceinline__ int part(int h, int i) { return KV4 ? h * N + i : 2 * i + h; }
-  __device__ __forceinline__ void load(const void* row, int h) {
+  static constexpr int kRow = D * (BF16 ? 2 : 4);  // bytes of a row
+  static __device__ __forceinline__ unsigned lane_offset(int row, int h) { return row * kRow + 16 * part(h, 0); }
+  // from a uniform address and lane_offset()
+  __device__ __forceinline__ void load(const void* base, unsigned off) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = static_cast<const Part*>(row)[part(h, i)];
+    for (int i = 0; i < N; ++i)
+      x[i] = *reinterpret_cast<const Part*>(static_cast<const char*>(base) + off + 16 * (KV4 ? i : 2 * i));
   }
 };
 
@@ -59,22 +65,21 @@ struct Operand {
 template <int D>
 struct Codes {
   u32x4 c[D / 64];
-  unsigned scale[D / 64];
-  __device__ __forceinline__ void load(const unsigned char* codes, const unsigned char* scales, size_t row, int h) {
-    const u32x4* p = reinterpret_cast<const u32x4*>(codes + row * (D / 2) + h * (D / 4));
-    const unsigned char* s = scales + row * (D / 32) + h * (D / 64);
+  unsigned scale;
+  static __device__ __forceinline__ unsigned lane_offset(int row, int h) { return row * (D / 2) + h * (D / 4); }
+  static __device__ __forceinline__ unsigned lane_scale(int row, int h) { return row * (D / 32) + h * (D / 64); }
+  __device__ __forceinline__ void load(const unsigned char* codes, const unsigned char* scales, unsigned off, unsigned soff) {
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      c[i] = p[i];
-      scale[i] = s[i];
-    }
+    for (int i = 0; i < D / 64; ++i) c[i] = *reinterpret_cast<const u32x4*>(codes + off + 16 * i);
+    if constexpr (D == 128) scale = *reinterpret_cast<const unsigned short*>(scales + soff);
+    else scale = scales[soff];
   }
   template <bool BF16>
   __device__ __forceinline__ void values(Operand<D, BF16, true>& k) const {
 #pragma unroll
     for (int w = 0; w < D / 16; ++w) {  // eight dims
       const unsigned code = c[w / 4][w % 4];
-      const float f = __builtin_bit_cast(float, scale[w / 4] << 23);
+      const float f = __builtin_bit_cast(float, (scale >> (8 * (w / 4)) & 255u) << 23);
       if constexpr (BF16) {
         const u32x4 v = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, f, 0)),
                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, f, 1)),
@@ -111,13 +116,16 @@ __device__ __forceinline__ f32x16 scores(const Operand<D, BF16, KV4>& q, const O
 template <int D, bool BF16, bool KV4>
 __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams p) {
   using Op = Operand<D, BF16, KV4>;
-  constexpr int KB = BF16 ? 2 : 1;                         // 32-key blocks of a wave at a time
-  constexpr int RB = D * (BF16 ? 2 : 4), CH = RB / 16;     // bytes and 16-byte chunks of a query
+  using Next = std::conditional_t<KV4, Codes<D>, Op>;
+  constexpr int KB = BF16 ? 2 : 1;                     // 32-key blocks of a wave at a time
+  constexpr int RB = Op::kRow, CH = RB / 16;           // bytes and 16-byte chunks of a query
+  constexpr int LB = RB + 16;  // ... and its stride in LDS: 16 rows at one chunk lie in 16 different bank groups
   constexpr int kRows = 65536 / RB < 256 ? 65536 / RB : 256;  // queries in LDS
-  __shared__ __attribute__((aligned(16))) u32x4 sQ[kRows * CH];
+  __shared__ __attribute__((aligned(16))) char sQ[kRows * LB];
   __shared__ __attribute__((aligned(16))) float sOff[kRows];  // -lse in log2 units, -inf for padding rows
   __shared__ __attribute__((aligned(16))) int sPlace[kRows];  // the row's place: position ctx + place
-  __shared__ int sNode[64];
+  __shared__ int sRow[kRows];                                 // its query, -1 for padding rows
+  __shared__ int sTicket;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -141,18 +149,18 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
     const unsigned long long bad = __ballot(node < 0 || node >= p.n);
     rows = bad ? (int)__builtin_ctzll(bad) : 64;
   }
-  if (wave == 0) sNode[lane] = node;
 
   // slots that no row sees, the pieces of the sequence a share each
+  constexpr int kThreads = 64 * kWeighWaves;
   {
     const int first = min(ctx, 64 * tm.head), gap = min(ctx, 64 * (tm.head + tm.skip)) - first;
     const int from = first + (int)((long long)gap * pc.index / pc.count);
     const int to = first + (int)((long long)gap * (pc.index + 1) / pc.count);
-    for (int j = from + tid; j < to; j += 64 * kWeighWaves) out[j] = p.decay > 0.f ? p.decay * old[j] : 0.f;
+    for (int j = from + tid; j < to; j += kThreads) out[j] = p.decay > 0.f ? p.decay * old[j] : 0.f;
   }
 
-  // This wave's steps: blocks of 32 KB keys of the piece, in turn.  A step's keys are
-  // context slots, or in the tile behind them the path's own rows.
+  // Steps: blocks of 32 KB keys of the piece.  A step's keys are context slots,
+  // or in the tile behind them the path's own rows.
   constexpr int KEYS = 32 * KB, SPT = 64 / KEYS;  // steps of a tile
   const int r32 = lane & 31, h = lane >> 5;
   struct Step {
@@ -170,124 +178,196 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
   };
   // The next step's keys, or their codes (with codes the path's own keys are
   // loaded where they are used).
-  std::conditional_t<KV4, Codes<D>, Op> next[KB];
-  auto key_row = [&](const Step& s, int kb) __attribute__((always_inline)) {  // past the end: any valid row
-    return min(s.key0 + 32 * kb + r32, s.end - 1);
-  };
-  auto new_key = [&](const Step& s, int kb) __attribute__((always_inline)) {
-    const int n = __shfl(node, key_row(s, kb));
-    return static_cast<const char*>(p.k_new) + (((size_t)b * p.n + n) * p.hkv + g) * RB;
+  Next next[KB];
+  auto new_key = [&](const Step& s, int kb, Op& k) __attribute__((always_inline)) {
+    const int n = __shfl(node, min(s.key0 + 32 * kb + r32, s.end - 1));
+    const char* row = static_cast<const char*>(p.k_new) + (((size_t)b * p.n + n) * p.hkv + g) * RB;
+    k.load(row, Op::lane_offset(0, h));
   };
   auto load = [&](const Step& s) __attribute__((always_inline)) {
-    if (s.key0 >= s.end || (KV4 && s.is_new)) return;
+    if (s.key0 >= s.end) return;
+    if (s.is_new) {
+      if constexpr (!KV4) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) new_key(s, kb, next[kb]);
+      }
+      return;
+    }
+    const size_t row = head * p.cache.cap + s.key0;
+    const int last = min(KEYS, s.end - s.key0) - 1;  // >= 0; keys past it are its copies
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const size_t row = head * p.cache.cap + key_row(s, kb);
-      if constexpr (KV4) next[kb].load(p.cache.k, p.cache.k_scale, row, h);
-      else if (s.is_new) next[kb].load(new_key(s, kb), h);
-      else next[kb].load(p.cache.k + row * RB, h);
+      const int r = min(32 * kb + r32, last);
+      if constexpr (KV4)
+        next[kb].load(p.cache.k + row * (D / 2), p.cache.k_scale + row * (D / 32), Next::lane_offset(r, h), Next::lane_scale(r, h));
+      else
+        next[kb].load(p.cache.k + row * RB, Next::lane_offset(r, h));
     }
   };
-  if (wave < n_steps) load(step_at(wave));
 
   const int total = rows * p.group;
-  // 16-byte chunk c of query r in LDS: rows 16 apart share banks
-  auto chunk = [](int r, int c) __attribute__((always_inline)) {
-    return r * CH + (CH >= 16 ? c ^ (r & 15) : c ^ ((r >> 1) & 7));
-  };
+  constexpr int kBatch = 4;
   for (int r0 = 0; r0 == 0 || r0 < total; r0 += kRows) {
     const int n_rows = min(kRows, total - r0);
     const int padded = (n_rows + 31) / 32 * 32;
-    __syncthreads();  // sNode is written; the queries before are no longer read
-    for (int u = tid; u < padded * CH; u += 64 * kWeighWaves) {
-      const int r = u / CH, c = u % CH;
-      u32x4 v = {};
-      if (r < n_rows) {
-        const int i = (r0 + r) / p.group;
-        const size_t at = ((size_t)b * p.n + sNode[i]) * p.hq + (size_t)g * p.group + (r0 + r - i * p.group);
-        v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + at * RB + 16 * c);
-        if (c == 0) {
-          sOff[r] = -p.lse[at] * kLog2e;
-          sPlace[r] = i;
-        }
-      } else if (c == 0) {
-        sOff[r] = -__builtin_inff();
-        sPlace[r] = 0;
+    if (r0 > 0) __syncthreads();  // the queries before are no longer read
+    // The rows' places, a row a thread; then their queries, kBatch 16-byte chunks
+    // a thread in flight at once, and behind the first of these (loads arrive in
+    // order) the first step's keys.
+    static_assert(kRows <= kThreads, "a row a thread");
+    float lse = __builtin_inff();
+    {
+      const int i = min(r0 + tid, max(total - 1, 0)) / p.group;
+      const int node_i = path ? __shfl(node, i) : i;
+      const int at = (b * p.n + node_i) * p.hq + g * p.group + (r0 + tid - i * p.group);
+      if (tid < n_rows) lse = p.lse[at];
+      if (tid < kRows) {
+        sPlace[tid] = i;
+        sRow[tid] = tid < n_rows ? at : -1;
       }
-      sQ[chunk(r, c)] = v;
+      if (tid == 0) sTicket = kWeighWaves;
     }
     __syncthreads();
-    for (int s = wave; s < n_steps; s += kWeighWaves) {
+    int s = wave;  // the first step; the others by ticket
+    for (int u0 = 0; u0 < padded * CH || u0 == 0; u0 += kBatch * kThreads) {
+      u32x4 v[kBatch];
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x) {
+        const int u = u0 + x * kThreads + tid, r = u / CH, c = u % CH;
+        const int row = r < padded ? sRow[r] : -1;
+        v[x] = u32x4{};
+        if (row >= 0) v[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (size_t)row * RB + 16 * c);
+      }
+      if (u0 == 0 && s < n_steps) load(step_at(s));
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x) {
+        const int u = u0 + x * kThreads + tid, r = u / CH, c = u % CH;
+        if (r < padded) *reinterpret_cast<u32x4*>(sQ + r * LB + 16 * c) = v[x];
+      }
+    }
+    if (tid < kRows) sOff[tid] = -lse * kLog2e;
+    __syncthreads();
+    while (s < n_steps) {
       const Step st = step_at(s);
       Op k[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         if constexpr (KV4) {
-          if (!st.is_new) next[kb].template values<BF16>(k[kb]);
-          else if (st.key0 < st.end) k[kb].load(new_key(st, kb), h);
+          if (!st.is_new) {
+            next[kb].template values<BF16>(k[kb]);
+          } else if (st.key0 < st.end) {
+            new_key(st, kb, k[kb]);
+            // waited for here: otherwise the compiler waits for every load, the
+            // next step's too, wherever the keys are used
+            __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0)
+          }
         } else {
           k[kb] = next[kb];
         }
       }
-      // the next step's keys, past the last one the first's for the next rows
-      if (s + kWeighWaves < n_steps) load(step_at(s + kWeighWaves));
-      else if (r0 + kRows < total) load(step_at(wave));
+      // The slot that this lane writes and its old weight (or the sum over the
+      // rows before), read ahead of the next step's keys, since loads arrive in
+      // order, and by every lane, since a wait stands behind a conditional one.
+      const int mine = st.key0 + r32 + (KB == 2 ? 32 * h : 0);
+      const int slot = st.is_new ? ctx + mine : mine;
+      const bool writes = mine < st.end && slot < p.cache.cap && (KB == 2 || h == 0);
+      const float keep = r0 > 0 ? 1.f : st.is_new ? 0.f : p.decay;
+      const float before = (r0 > 0 || p.decay == 0.f ? out : old)[min(slot, p.cache.cap - 1)];
+      int ticket = 0;
+      if (lane == 0) ticket = atomicAdd(&sTicket, 1);
+      s = __builtin_amdgcn_readfirstlane(ticket);
+      if (s < n_steps) load(step_at(s));
       if (st.key0 >= st.end) continue;
-      // the places of the rows that see the lane's key of each block
-      int from[KB], to[KB];
-      bool all = !st.is_new;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const int key = st.key0 + 32 * kb + r32;
-        const int slot = st.is_new ? ctx + key : key;
-        from[kb] = st.is_new ? key : 0;
-        const long long last = (long long)slot - ctx + p.plan.window - 1;
-        to[kb] = slot < p.plan.n_sinks || last > 64 ? 64 : (int)last;
-      }
-      all = all && (st.key0 + KEYS <= p.plan.n_sinks || st.key0 >= ctx + rows - p.plan.window);
       float sum[KB][2] = {};
-      for (int rt = 0; rt < padded; rt += 32) {
-        Op q;
+      // a step whose keys every row sees needs no places
+      const bool all = !st.is_new && (st.key0 + KEYS <= p.plan.n_sinks || st.key0 >= ctx + rows - p.plan.window);
+      auto walk = [&](auto ALL_) __attribute__((always_inline)) {
+        constexpr bool ALL = decltype(ALL_)::value;
+        int from[KB], to[KB];  // the places of the rows that see the lane's key of each block
+        if (!ALL) {
 #pragma unroll
-        for (int i = 0; i < Op::N; ++i) q.x[i] = __builtin_bit_cast(typename Op::Part, sQ[chunk(rt + r32, Op::part(h, i))]);
-        f32x4 off[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) off[x] = *reinterpret_cast<const f32x4*>(&sOff[rt + 8 * x + 4 * h]);
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const f32x16 z = scores<D, BF16, KV4>(q, k[kb]);
-          if (all) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x)
-              sum[kb][x & 1] += __builtin_amdgcn_exp2f(fmaf(z[x], p.scale_log2, off[x >> 2][x & 3]));
-          } else {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const int place = sPlace[rt + 8 * (x >> 2) + 4 * h + (x & 3)];
-              const float e = __builtin_amdgcn_exp2f(fmaf(z[x], p.scale_log2, off[x >> 2][x & 3]));
-              sum[kb][x & 1] += place >= from[kb] && place <= to[kb] ? e : 0.f;
-            }
+          for (int kb = 0; kb < KB; ++kb) {
+            const int key = st.key0 + 32 * kb + r32;
+            const int at = st.is_new ? ctx + key : key;
+            from[kb] = st.is_new ? key : 0;
+            const long long last = (long long)at - ctx + p.plan.window - 1;
+            to[kb] = at < p.plan.n_sinks || last > 64 ? 64 : (int)last;
           }
         }
+        Op q;
+        f32x4 off[4];
+        const unsigned lane_q = r32 * LB + 16 * Op::part(h, 0);
+        auto query = [&](int rt, int i) __attribute__((always_inline)) {
+          q.x[i] = *reinterpret_cast<const typename Op::Part*>(sQ + rt * LB + lane_q + 16 * (KV4 ? i : 2 * i));
+        };
+        auto offset = [&](int rt, int x) __attribute__((always_inline)) {
+          off[x] = *reinterpret_cast<const f32x4*>(&sOff[rt + 8 * x + 4 * h]);
+        };
+        auto add = [&](const f32x16& z, int rt, int kb, int x) __attribute__((always_inline)) {
+          float e = __builtin_amdgcn_exp2f(fmaf(z[x], p.scale_log2, off[x >> 2][x & 3]));
+          if (!ALL) {
+            const int place = sPlace[rt + 8 * (x >> 2) + 4 * h + (x & 3)];
+            e = place >= from[kb] && place <= to[kb] ? e : 0.f;
+          }
+          sum[kb][x & 1] += e;
+        };
+#pragma unroll
+        for (int i = 0; i < Op::N; ++i) query(0, i);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) offset(0, x);
+        if constexpr (KB == 2) {
+          // Matrix and vector instructions in turn: the products of one block
+          // between the exponentials of the other, operands reloaded as soon as
+          // they are used.  (With the products first and the exponentials behind
+          // them the two took turns on the SIMD as well: 62 us instead of 4..)
+          constexpr int E = 16 / Op::N;  // exponentials a product
+          f32x16 z0 = scores<D, BF16, KV4>(q, k[0]), z1;
+          for (int rt = 0; rt < padded; rt += 32) {
+            const int nt = rt + 32 < padded ? rt + 32 : 0;
+#pragma unroll
+            for (int i = 0; i < Op::N; ++i) {
+              z1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q.x[i], k[1].x[i], i == 0 ? f32x16{} : z1, 0, 0, 0);
+              query(nt, i);
+#pragma unroll
+              for (int x = E * i; x < E * i + E; ++x) add(z0, rt, 0, x);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < Op::N; ++i) {
+              z0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q.x[i], k[0].x[i], i == 0 ? f32x16{} : z0, 0, 0, 0);
+#pragma unroll
+              for (int x = E * i; x < E * i + E; ++x) add(z1, rt, 1, x);
+              if (E * i % 4 + E >= 4) offset(nt, E * i / 4);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        } else {
+          for (int rt = 0; rt < padded; rt += 32) {
+            const int nt = rt + 32 < padded ? rt + 32 : 0;
+            const f32x16 z = scores<D, BF16, KV4>(q, k[0]);
+#pragma unroll
+            for (int i = 0; i < Op::N; ++i) query(nt, i);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) add(z, rt, 0, x);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) offset(nt, x);
+          }
+        }
+      };
+      if (padded > 0) {
+        if (all) walk(std::true_type{});
+        else walk(std::false_type{});
       }
       // both halves of a key's rows; with two blocks each half stores one
       float w;
-      int key = st.key0 + r32;
       if constexpr (KB == 2) {
         const float a = sum[0][0] + sum[0][1], c = sum[1][0] + sum[1][1];
         w = (h ? c : a) + __shfl_xor(h ? a : c, 32);
-        key += 32 * h;
       } else {
         w = sum[0][0] + sum[0][1];
         w += __shfl_xor(w, 32);
-        if (h) continue;
       }
-      if (key >= st.end) continue;
-      const int slot = st.is_new ? ctx + key : key;
-      if (slot >= p.cache.cap) continue;
-      if (r0 > 0) w += out[slot];
-      else if (!st.is_new && p.decay > 0.f) w = fmaf(p.decay, old[slot], w);
-      out[slot] = w;
+      if (writes) out[slot] = keep > 0.f ? fmaf(keep, before, w) : w;
     }
   }
 }
@@ -302,7 +382,7 @@ void launch(const WeighParams& p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_weigh(const WeighParams& params, bool bf16, hipStream_t s, hipEvent_t ev0, hipEvent_t ev1) {
-  // two workgroups a compute unit, a tile a wave at least
+  // a workgroup a compute unit
   WeighParams p = params;
   p.plan = {};
   p.plan.batch = p.batch;
@@ -310,9 +390,9 @@ hipError_t launch_weigh(const WeighParams& params, bool bf16, hipStream_t s, hip
   p.plan.ctx_lens = p.cache.lens;
   p.plan.n_sinks = p.n_sinks;
   p.plan.window = p.window;
-  const int per_g = 512 / p.hkv;
+  const int per_g = 256 / p.hkv;
   p.plan.slots_per_g = per_g > p.batch ? per_g : p.batch;
-  p.plan.min_tiles = kWeighWaves;
+  p.plan.min_tiles = 1;
   p.plan.tiles_rg = 5;  // (least_piece: no more than four)
   if (ev0) (void)hipEventRecord(ev0, s);
   if (p.d == 128) {
