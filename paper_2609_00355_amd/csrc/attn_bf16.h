@@ -247,19 +247,26 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   // V(1)).  Barrier t needs K(t) and V(t - 1), both of group t - 3, so before
   // it the wave waits until at most its groups t - 2 and t - 1 are in flight
   // (vmcnt counts a wave's loads in issue order; 2 kLoads a group).
+  //
+  // The woven schedule reads V(t) in step t + 2 instead, so everything said of V
+  // is said of the tile before: group t is K(t + 3) and V(t + 1), over V(t - 3),
+  // and barrier t needs K(t) and V(t - 2).
+  constexpr int kVAhead = WIN ? 1 : 2;
   auto ring_issue = [&](int t) __attribute__((always_inline)) {
     if (t + 3 < n_tiles) issue(t + 3, false);
-    if (t + 2 < n_tiles) issue(t + 2, true);
+    if (t + kVAhead < n_tiles) issue(t + kVAhead, true);
   };
   auto ring_prologue = [&]() __attribute__((always_inline)) {
     issue(0, false);                    // group -3: K(0)
     if (n_tiles > 1) issue(1, false);   // group -2: K(1), V(0)
-    issue(0, true);
+    if (!WIN) issue(0, true);
     if (n_tiles > 2) issue(2, false);   // group -1: K(2), V(1)
-    if (n_tiles > 1) issue(1, true);
+    if (WIN) issue(0, true);
+    else if (n_tiles > 1) issue(1, true);
   };
   auto ring_wait = [&](int t) __attribute__((always_inline)) {
     if (t + 2 >= n_tiles) wait_vmcnt<0>();
+    else if (WIN && t == 0) wait_vmcnt<KV4 ? 0 : 3 * kLoads>();  // group -2 is K(1) alone
     else wait_vmcnt<KV4 ? 0 : 4 * kLoads>();
   };
 
@@ -329,9 +336,10 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   // dims) while its neighbour on the SIMD, alone there, computes; shared by all
   // waves, that work took 50 vector instructions a tile from each.
   // The tile of new keys, which is dense, comes by DMA: K at step tn - 2, V at step
-  // tn - 1 (or in the prologue) into the stages that the codes would take, whose
-  // stores go one stage further instead (K(t - 1)'s or V(t - 2)'s, free since
-  // barrier t); every loading wave waits for it before barrier tn.
+  // tn - 1 (or in the prologue) into the stages that the codes would take. Their
+  // store of K goes one stage further instead (K(t - 1)'s, free since barrier t),
+  // that of V, which has no free stage, is left out; every loading wave waits for
+  // the tile before barrier tn.
   constexpr int CPL = CH / stride;  // chunks of a lane, 4 bytes of codes each
   constexpr int SPL = CPL > 4 ? CPL / 4 : 1;  // scales of a lane
   struct Codes {
@@ -395,14 +403,14 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
       if (tn == 0) issue(tn, true);
       codes_store(0, false, k0);
       codes_store(1, false, k1);
-      codes_store(0, true, v0);
+      if (tn != 0) codes_store(0, true, v0);
     }
     auto step = [&](int t, auto P_) __attribute__((always_inline)) {
       constexpr int P = decltype(P_)::value;
       if (t == tn) wait_vmcnt<0>();
       lds_barrier();
       codes_store(t + 2, false, cK[P]);
-      codes_store(t + 1, true, cV[P]);
+      if (t + 1 != tn) codes_store(t + 1, true, cV[P]);
       codes_load(t + 4, false, cK[P]);
       codes_load(t + 3, true, cV[P]);
       if (t + 2 == tn) issue(tn, false);
@@ -551,36 +559,11 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   // probability sum passes kSumLimit (a score more than log2(kSumLimit) / c
   // above the reference) or there is no reference yet: O and l are rescaled
   // and the tile's probabilities redone.
-  //
-  // A window masks context tiles too: those at its far end, where the rows'
-  // first keys differ, and the last one of the sinks.  A tile may then hold no
-  // key that a row sees, and the row's reference stays at -inf.
   auto yphase = [&](int t) __attribute__((always_inline)) {
     const int j = tb + t;
     const bool is_new = j == ct;
-    const int key0 = is_new ? 0 : key_of(j);
-    const int nvalid = is_new ? p.n : min(64, ctx - key0);
-    const bool edge = WIN && !is_new && key0 + 64 > p.n_sinks && key0 < ctx + p.n - p.window;
-    if (WIN && (is_new || nvalid < 64 || edge)) {
-      unsigned long long vis = bits_below(nvalid);
-      int lane_ = lane;
-      asm volatile("" : "+v"(lane_));
-      const int row_ = 32 * (rgi * p.tiles_rg + wave) + (lane_ & 31);
-      if (row_ < p.rows) {
-        const int node_ = row_ / p.group;
-        if (TREE && is_new) vis &= sAnc[node_];
-        if (edge) vis &= window_word(p.n_sinks, ctx + (TREE ? sDepth[node_] : node_) - p.window + 1, key0);
-      }
-      vis >>= 4 * h;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int jj = 0; jj < 4; ++jj)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!((vis >> (32 * kb + 8 * jj + i)) & 1ull)) S[kb][4 * jj + i] = kNegInf;
-    }
-    if (!WIN && (is_new || nvalid < 64)) {
+    const int nvalid = is_new ? p.n : min(64, ctx - 64 * j);
+    if (is_new || nvalid < 64) {
       unsigned long long anc = ~0ull;
       if (TREE && is_new) {  // the row's node, worked out here for the same reason as at the end
         int lane_ = lane;
@@ -616,7 +599,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
       const float m_new = fmaxf(m_run, mx);
       const float m_use = m_new == kNegInf ? 0.f : m_new;
       const float alpha = __builtin_amdgcn_exp2f((m_run - m_use) * c);
-      m_run = WIN ? m_new : m_use;
+      m_run = m_use;
       nmc = -m_use * c;
       l_run *= alpha;
 #pragma unroll
@@ -670,6 +653,133 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
 #endif
   };
 
+  // The woven schedule (WIN).  Step t, after barrier t, runs P.V of tile t - 2 with
+  // the softmax of tile t - 1 between its products, then Q.K^T of tile t with the
+  // softmax's rest.  A wave's matrix and vector instructions thus alternate, where
+  // in the other schedule the two waves of a SIMD, which every barrier lines up,
+  // go through the matrix phase and then the softmax together.  Registers are the
+  // same: the products of 16 keys of tile t - 2 come before the probabilities of
+  // tile t - 1 that take their place in Pw, and all of the softmax that reads a
+  // block of scores before the products that overwrite it.
+  //
+  // mask_tile(t) masks the scores of tile t; piece i (of 16) turns two scores into
+  // probabilities against the reference.
+  auto mask_tile = [&](int t) __attribute__((always_inline)) {
+    const int j = tb + t;
+    const bool is_new = j == ct;
+    const int key0 = is_new ? 0 : key_of(j);
+    const int nvalid = is_new ? p.n : min(64, ctx - key0);
+    const bool edge = !is_new && key0 + 64 > p.n_sinks && key0 < ctx + p.n - p.window;
+    if (!(is_new || nvalid < 64 || edge)) return;
+    unsigned long long vis = bits_below(nvalid);
+    int lane_ = lane;
+    asm volatile("" : "+v"(lane_));
+    const int row_ = 32 * (rgi * p.tiles_rg + wave) + (lane_ & 31);
+    if (row_ < p.rows) {
+      const int node_ = row_ / p.group;
+      if (TREE && is_new) vis &= sAnc[node_];
+      if (edge) vis &= window_word(p.n_sinks, ctx + (TREE ? sDepth[node_] : node_) - p.window + 1, key0);
+    }
+    vis >>= 4 * h;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!((vis >> (32 * kb + 8 * jj + i)) & 1ull)) S[kb][4 * jj + i] = kNegInf;
+  };
+  float nmc_run = 0.f;  // -reference * c, 0 while there is none
+  auto piece = [&](int i, float& lsum) __attribute__((always_inline)) {
+    const int kb = i >> 3, x = 2 * (i & 7);
+    const bf16x2 w = {(__bf16)__builtin_amdgcn_exp2f(fmaf(S[kb][x], c, nmc_run)),
+                      (__bf16)__builtin_amdgcn_exp2f(fmaf(S[kb][x + 1], c, nmc_run))};
+    unsigned u = __builtin_bit_cast(unsigned, w);
+    asm volatile("" : "+v"(u));  // here and not where it is used: behind a branch, with 32 more registers
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+    lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u), ones, lsum, false);
+    Pw[kb][(i >> 2) & 1][i & 3] = u;
+  };
+  auto pv = [&](int u, int db, bf16x8 v) __attribute__((always_inline)) {
+    O[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, Pw[u >> 1][u & 1]), O[db], 0, 0, 0);
+  };
+  // Softmax of tile t against P.V of tile t - 1 (stage SV; if PV_), then Q.K^T of tile
+  // t + 1 (stage SK; if QK_).  A row's reference moves to its maximum when a
+  // score lies more than kFar above it in log2 units, or there is none yet.
+  auto woven = [&](int t, auto SK_, auto SV_, auto QK_, auto PV_, int ti) __attribute__((always_inline)) {
+    constexpr int SK = decltype(SK_)::value, SV = decltype(SV_)::value;
+    constexpr bool DO_QK = decltype(QK_)::value, DO_PV = decltype(PV_)::value;
+    constexpr int NV = 4 * DB, NK = 2 * KS, AH = kOperandsAhead, PP = 4 / DB;
+    constexpr float kFar = 8.f;
+    bf16x8 vr[NV], kr[NK];  // operands, AH ahead; Q.K^T takes one key block after the other
+    auto get_v = [&](int i) __attribute__((always_inline)) {
+      if (DO_PV && i < NV) vr[i] = load_v(i / DB, i % DB, SV);
+      else if (DO_QK && i >= NV && i < NV + NK) kr[i - NV] = load_k((i - NV) % KS, (i - NV) / KS, SK);
+    };
+    if (DO_PV) {
+#pragma unroll
+      for (int i = 0; i < AH; ++i) get_v(i);
+    }
+    mask_tile(t);
+    float mx = kNegInf;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {  // the first 16 keys, with the scores' maximum between
+      if (DO_PV) {
+        get_v(i + AH);
+        pv(0, i, vr[i]);
+      }
+#pragma unroll
+      for (int x = 32 / DB * i; x < 32 / DB * (i + 1); x += 2)
+        mx = __builtin_fmaxf(__builtin_fmaxf(S[x >> 4][x & 15], S[x >> 4][(x & 15) + 1]), mx);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float lsum = 0.f, alpha = 1.f;
+    const bool far = __builtin_amdgcn_ballot_w64((mx - m_run) * c > kFar) != 0;
+    if (far) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_new = fmaxf(m_run, mx);
+      const float m_use = m_new == kNegInf ? 0.f : m_new;
+      alpha = __builtin_amdgcn_exp2f((m_run - m_use) * c);
+      m_run = m_new;
+      nmc_run = -m_use * c;
+      l_run *= alpha;
+    }
+#pragma unroll
+    for (int i = DB; i < NV; ++i) {
+      if (DO_PV) {
+        if (i + AH < NV) get_v(i + AH);
+        pv(i / DB, i % DB, vr[i]);
+      }
+#pragma unroll
+      for (int x = PP * (i - DB); x < PP * (i - DB + 1); ++x) piece(x, lsum);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (far) {  // P.V of the tile before was against the old reference
+#pragma unroll
+      for (int db = 0; db < DB; ++db) O[db] *= alpha;
+    }
+    if (STAGED) {
+      if (ti >= 0) stage_step(ti, SK_);
+    } else if (RING) {
+      if (ti >= 0) ring_issue(ti);
+    }
+    if (DO_QK) {
+#pragma unroll
+      for (int i = NV; i < NV + AH; ++i) get_v(i);
+    }
+#pragma unroll
+    for (int i = 0; i < (DO_QK ? NK : 4); ++i) {
+      if (DO_QK) {
+        get_v(NV + i + AH);
+        const int kb = i / KS, ks = i % KS;
+        S[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[i], qf[ks], ks == 0 ? f32x16{} : S[kb], 0, 0, 0);
+      }
+      if (i < 4) piece(12 + i, lsum);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l_run += lsum;
+  };
+
   // Schedule.  X_t = {Q.K^T of tile t, P.V of tile t - 1}, Y_t = softmax of
   // tile t; every wave runs barrier 0, X_0 Y_0, barrier 1, X_1 Y_1, ...,
   // X_{n-1} Y_{n-1} and the last P.V.  All waves keep the same order: the two
@@ -696,28 +806,56 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   lds_barrier();  // barrier 0: K(0) has landed, the ancestor words are written
   if (RING) ring_issue(0);
   xphase(I0{}, YES{}, NO{}, STAGED ? 0 : -1);
-  auto step = [&](int t, auto SK_) __attribute__((always_inline)) {
-    yphase(t - 1);
-    if (RING) ring_wait(t);
-    lds_barrier();  // barrier t: K(t) and V(t - 1) have landed, and X_{t-1} has ended everywhere
-    // DMA by all waves: waves 0-3 issue right away, waves 4-6 halfway through
-    // X_t, so that of the two computing waves sharing a SIMD one computes while
-    // the other waits for the memory pipeline to take its loads
-    if (RING && wave < 4) ring_issue(t);
-    xphase(SK_, YES{}, YES{}, STAGED || wave >= 4 ? t : -1);
-  };
-  int t = 1;
-  while (t < n_tiles) {
-    step(t, I1{});
-    if (++t >= n_tiles) break;
-    step(t, I2{});
-    if (++t >= n_tiles) break;
-    step(t, I3{});
-    if (++t >= n_tiles) break;
-    step(t, I0{});
-    ++t;
+  if constexpr (WIN) {
+    auto step = [&](int t, auto SK_, auto SV_, auto PV_) __attribute__((always_inline)) {
+      if (RING) ring_wait(t);
+      lds_barrier();  // barrier t: K(t) and V(t - 2) have landed, and step t - 1 has ended everywhere
+      if (RING && wave < 4) ring_issue(t);
+      woven(t - 1, SK_, SV_, YES{}, PV_, STAGED || wave >= 4 ? t : -1);
+    };
+    if (n_tiles > 1) step(1, I1{}, I3{}, NO{});
+    for (int t = 2; t < n_tiles;) {
+      step(t, I2{}, I0{}, YES{});
+      if (++t >= n_tiles) break;
+      step(t, I3{}, I1{}, YES{});
+      if (++t >= n_tiles) break;
+      step(t, I0{}, I2{}, YES{});
+      if (++t >= n_tiles) break;
+      step(t, I1{}, I3{}, YES{});
+      ++t;
+    }
+    // the last softmax with P.V of the tile before, then the last P.V
+    if (n_tiles == 1) woven(0, I0{}, I0{}, NO{}, NO{}, -1);
+    else switch (n_tiles & 3) {
+      case 2: woven(n_tiles - 1, I0{}, I0{}, NO{}, YES{}, -1); break;
+      case 3: woven(n_tiles - 1, I0{}, I1{}, NO{}, YES{}, -1); break;
+      case 0: woven(n_tiles - 1, I0{}, I2{}, NO{}, YES{}, -1); break;
+      default: woven(n_tiles - 1, I0{}, I3{}, NO{}, YES{}, -1); break;
+    }
+  } else {
+    auto step = [&](int t, auto SK_) __attribute__((always_inline)) {
+      yphase(t - 1);
+      if (RING) ring_wait(t);
+      lds_barrier();  // barrier t: K(t) and V(t - 1) have landed, and X_{t-1} has ended everywhere
+      // DMA by all waves: waves 0-3 issue right away, waves 4-6 halfway through
+      // X_t, so that of the two computing waves sharing a SIMD one computes while
+      // the other waits for the memory pipeline to take its loads
+      if (RING && wave < 4) ring_issue(t);
+      xphase(SK_, YES{}, YES{}, STAGED || wave >= 4 ? t : -1);
+    };
+    int t = 1;
+    while (t < n_tiles) {
+      step(t, I1{});
+      if (++t >= n_tiles) break;
+      step(t, I2{});
+      if (++t >= n_tiles) break;
+      step(t, I3{});
+      if (++t >= n_tiles) break;
+      step(t, I0{});
+      ++t;
+    }
+    yphase(n_tiles - 1);
   }
-  yphase(n_tiles - 1);
   switch (n_tiles & 3) {  // P.V of the last tile, stage (n_tiles - 1) % 4
     case 1: xphase(I1{}, NO{}, YES{}, -1); break;
     case 2: xphase(I2{}, NO{}, YES{}, -1); break;
