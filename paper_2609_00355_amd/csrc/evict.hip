@@ -3,15 +3,20 @@
 // Of every (sequence, KV head) with more than `budget` slots the first n_sinks,
 // the last n_recent and the budget - n_sinks - n_recent of greatest weight
 // among the others are kept, in their order; ties go to the lowest slot and a
-// NaN counts as larger than every number.  Two launches:
+// NaN counts as larger than every number.
 //
-// 1. evict_select, one workgroup per (sequence, KV head): the least kept weight
-//    by radix selection on order-preserving keys, then the kept slots in order
-//    by prefix sums.  The first count takes 11 bits (sign, exponent and two of
-//    the fraction), which leaves few enough keys to go on with in LDS.  Bound
-//    by latency: one read of the weights and about fifteen barriers.
-// 2. evict_gather: the kept rows of K, V, scales and weights, 16 bytes a lane
-//    where rows are that wide.  Bound by memory.
+// Selection, by a workgroup of a (sequence, KV head): the least kept weight by
+// radix selection on order-preserving keys, then the kept slots in order by prefix
+// sums.  The first count takes 11 bits (sign, exponent and two of the fraction),
+// which leaves few enough keys to go on with in LDS.  Bound by latency: one read
+// of the weights and about fifteen barriers.  Then the kept rows of K, V, scales
+// and weights are copied, 16 bytes a lane, bound by memory.
+//
+// Where LDS holds every key of the cache, the workgroups of a head (as many as
+// fill the compute units) all select, which costs no more time than one doing so,
+// and each copies its share of the rows: one launch.  Longer caches' selection
+// reads the weights several times: one workgroup does it and a second launch
+// copies.
 #include "glance_internal.h"
 
 #include "attn_plan.h"
@@ -51,6 +56,52 @@ __device__ __forceinline__ int row_incl_sum(int v) {
 }
 static_assert(kSelectWaves == 16, "a row of lanes holds the waves' counts");
 
+// The rows r0 .. r1 - 1 of a head's destination, by a workgroup of
+// kSelectThreads; slot_of(r) is the source slot of row r.
+template <class Slot>
+__device__ __forceinline__ void gather_rows(const EvictParams& p, int head, int r0, int r1, Slot slot_of) {
+  constexpr int kBatch = 4;  // 16-byte pieces of a thread in flight
+  const int tid = threadIdx.x;
+  const int shift = __builtin_ctz((unsigned)p.src.row_bytes / 16);  // pieces of a row: a power of two
+  const int units = r1 > r0 ? (r1 - r0) << shift : 0;
+  const size_t from = (size_t)head * p.src.cap, to = (size_t)head * p.dst.cap;
+  for (int u0 = 0; u0 < 2 * units; u0 += kBatch * kSelectThreads) {
+    u32x4 v[kBatch];
+    u32x4* at[kBatch];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      const int u = min(u0 + x * kSelectThreads + tid, 2 * units - 1);
+      const bool v_side = u >= units;
+      const int w = v_side ? u - units : u;
+      const int row = r0 + (w >> shift), piece = w & ((1 << shift) - 1);
+      const u32x4* src = reinterpret_cast<const u32x4*>(v_side ? p.src.v : p.src.k);
+      u32x4* dst = reinterpret_cast<u32x4*>(v_side ? p.dst.v : p.dst.k);
+      v[x] = src[((from + slot_of(row)) << shift) + piece];
+      at[x] = dst + ((to + row) << shift) + piece;
+    }
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x)
+      if (u0 + x * kSelectThreads + tid < 2 * units) *at[x] = v[x];
+  }
+  for (int r = r0 + tid; r < r1; r += kSelectThreads) {
+    const size_t f = from + slot_of(r), t = to + r;
+    const float w = p.src.weights[f];
+    if (p.src.kv4) {
+      if (p.d == 128) {  // 4 or 2 bytes of scales
+        const unsigned k = reinterpret_cast<const unsigned*>(p.src.k_scale)[f], v = reinterpret_cast<const unsigned*>(p.src.v_scale)[f];
+        reinterpret_cast<unsigned*>(p.dst.k_scale)[t] = k;
+        reinterpret_cast<unsigned*>(p.dst.v_scale)[t] = v;
+      } else {
+        const unsigned short k = reinterpret_cast<const unsigned short*>(p.src.k_scale)[f], v = reinterpret_cast<const unsigned short*>(p.src.v_scale)[f];
+        reinterpret_cast<unsigned short*>(p.dst.k_scale)[t] = k;
+        reinterpret_cast<unsigned short*>(p.dst.v_scale)[t] = v;
+      }
+    }
+    p.dst.weights[t] = w;
+  }
+}
+
+template <bool GATHER>
 __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   __shared__ u32x4 s_keys[kHeld / 4];
   __shared__ unsigned s_hist[kBins];
@@ -61,9 +112,18 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = clamp_len(p.src.lens[b], p.src.cap);
+  // the places that this workgroup fills
+  const int r0 = GATHER ? (int)((long long)p.budget * blockIdx.y / gridDim.y) : 0;
+  const int r1 = GATHER ? (int)((long long)p.budget * (blockIdx.y + 1) / gridDim.y) : p.budget;
   int* kept = p.kept + (size_t)head * p.budget;
+  int* s_kept = reinterpret_cast<int*>(s_keys);  // GATHER: the slots at those places
+  if (GATHER && head % p.hkv == 0 && blockIdx.y == 0 && tid == 0) p.dst.lens[b] = min(len, p.budget);
   if (len <= p.budget) {
-    for (int j = tid; j < p.budget; j += kSelectThreads) kept[j] = j < len ? j : -1;
+    for (int j = r0 + tid; j < r1; j += kSelectThreads) kept[j] = j < len ? j : -1;
+    if (GATHER) {
+      const int from = (int)((long long)len * blockIdx.y / gridDim.y), to = (int)((long long)len * (blockIdx.y + 1) / gridDim.y);
+      gather_rows(p, head, from, to, [&](int r) { return r; });
+    }
     return;
   }
   const float* w = p.src.weights + (size_t)head * p.src.cap;
@@ -243,9 +303,20 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
       int place = out + half(at, c);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (keep[c] >> i & 1u) kept[place++] = j + i;
+        if (keep[c] >> i & 1u) {
+          // (a place is at most its slot, and the barrier in scan() lies behind
+          // every read of the keys up to this chunk's: none is overwritten unread)
+          if (!GATHER) kept[place] = j + i;
+          else if (place >= r0 && place < r1) s_kept[place - r0] = j + i;
+          ++place;
+        }
       out += half(total, c);
     }
+  }
+  if (GATHER) {
+    __syncthreads();
+    for (int r = r0 + tid; r < r1; r += kSelectThreads) kept[r] = s_kept[r - r0];
+    gather_rows(p, head, r0, r1, [&](int r) { return s_kept[r - r0]; });
   }
 }
 
@@ -288,7 +359,17 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t s, hipEvent_t ev0, hip
   const long long units = (long long)p.budget * (p.src.row_bytes / 16);
   const dim3 grid((unsigned)((units + kGatherThreads - 1) / kGatherThreads), (unsigned)heads, 2);
   if (ev0) (void)hipEventRecord(ev0, s);
-  hipLaunchKernelGGL(evict_select, dim3((unsigned)heads), dim3(kSelectThreads), 0, s, p);
+  // shared lengths: other workgroups of the one launch still read what it writes
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p.src.lens), b = reinterpret_cast<uintptr_t>(p.dst.lens);
+  const bool apart = (a > b ? a - b : b - a) >= (size_t)p.batch * sizeof(int);
+  if (p.src.cap <= kHeld && apart) {
+    const int parts = heads < 256 ? 256 / heads : 1;
+    hipLaunchKernelGGL(evict_select<true>, dim3((unsigned)heads, (unsigned)parts), dim3(kSelectThreads), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (ev1) (void)hipEventRecord(ev1, s);
+    return e;
+  }
+  hipLaunchKernelGGL(evict_select<false>, dim3((unsigned)heads), dim3(kSelectThreads), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess) {
     hipLaunchKernelGGL(evict_gather, grid, dim3(kGatherThreads), 0, s, p);

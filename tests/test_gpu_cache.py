@@ -369,6 +369,30 @@ def test_evict_from_long_contexts():
         assert to.v[b, 0, :, 63].cpu().tolist() == [float(x) for x in want[b][0]]
 
 
+def test_evict_with_every_key_held():
+    """The longest caches whose keys the selection holds: few heads with many workgroups each, and shares that end inside a chunk."""
+    lens, cap = [32768, 30000, 17], 32768
+    g = torch.Generator().manual_seed(4)
+    w = torch.rand(3, 2, cap, generator=g)
+    w[1] = (w[1] * 4).floor() / 4
+    k = torch.arange(cap, dtype=torch.float32).reshape(1, 1, -1, 1).expand(3, 2, -1, 64).contiguous().cuda()
+    src = G.ContextCache(k, k + 0.5, torch.tensor(lens, dtype=torch.int32).cuda(), weights=w.cuda())
+    for budget, n_sinks, n_recent in ((9001, 10, 700), (32767, 0, 0), (3, 1, 1), (5000, 2000, 3000)):
+        to = G.new_cache(3, 2, budget, 64, dtype=torch.float32, weights=True)
+        kept = G.glance_cache_evict(src, to, budget, n_sinks, n_recent)
+        torch.cuda.synchronize()
+        want = OC.evict(lens, w.numpy(), budget, n_sinks, n_recent)
+        assert to.ctx_lens.cpu().tolist() == [min(x, budget) for x in lens]
+        for b in range(3):
+            for h in range(2):
+                slots = want[b][h]
+                assert kept[b, h].cpu().tolist() == slots + [-1] * (budget - len(slots))
+                assert to.k[b, h, :len(slots), 0].cpu().tolist() == [float(x) for x in slots]
+                assert to.v[b, h, :len(slots), 63].cpu().tolist() == [x + 0.5 for x in slots]
+                assert torch.equal(to.weights[b, h, :len(slots)].cpu(), w[b, h][slots])
+                assert (to.k[b, h, len(slots):] == 0).all()
+
+
 def test_evict_with_shared_lengths():
     c = Case("bf16", "dense", 64, 1, 2, 2, [200, 30], seed=1, weights=True)
     to = G.new_cache(2, 2, 64, 64, weights=True)
@@ -378,6 +402,57 @@ def test_evict_with_shared_lengths():
     assert to.ctx_lens.cpu().tolist() == [64, 30]
     want = OC.evict([200, 30], c.weights.numpy(), 64, 1, 2)
     assert kept[0, 1].cpu().tolist() == want[0][1] and kept[1, 0, :30].cpu().tolist() == list(range(30))
+
+
+# ------------------------------------------------------------- long caches
+@pytest.mark.parametrize("fmt,dtype,d,hkv,cap", [("dense", "bf16", 128, 2, 2 ** 24 + 3), ("dense", "f32", 64, 2, 2 ** 24 + 3),
+                                                 ("kv4", "bf16", 128, 4, 2 ** 25), ("kv4", "f32", 128, 4, 2 ** 25)])
+def test_offsets_past_32_bits(fmt, dtype, d, hkv, cap):
+    """The last slots of a cache of more than 8 GB: what a window and the sinks see there equals a short cache of those slots."""
+    sinks, window, n, last = 3, 500, 20, 600
+    c = Case(dtype, fmt, d, n, 2 * hkv, hkv, [sinks + last], seed=cap % 97, weights=True)
+    ctx = cap - 8
+    big = G.new_cache(1, hkv, cap, d, dtype=DT[dtype], fmt=fmt, weights=True)
+    for t, s in ((big.k, c.cache.k), (big.v, c.cache.v), (big.k_scale, c.cache.k_scale), (big.v_scale, c.cache.v_scale)):
+        if t is not None:
+            t[:, :, :sinks], t[:, :, ctx - last:ctx] = s[:, :, :sinks], s[:, :, sinks:]
+    big.ctx_lens.fill_(ctx)
+    big.weights.fill_(1.0)
+    c.cache = big
+    out, lse = c.check(True, sinks, window)
+    block = c.check(False, sinks, window)[1]
+    G.glance_cache_weigh(c.q.cuda(), big, block, decay=0.5, n_sinks=sinks, window=window)
+    torch.cuda.synchronize()
+    ref = OC.weigh(c.q.double(), c.k64, block.double().cpu(), c.lens, np.ones((1, hkv, sinks + last)), 0.5, n_sinks=sinks, window=window)
+    got = _np(torch.cat([big.weights[:, :, :sinks], big.weights[:, :, ctx - last:ctx]], dim=2))
+    assert (np.abs(got - ref) <= _weight_bound(c, _np(block), 2 * n, ref)).all()
+    assert (big.weights[:, :, sinks:ctx - last] == 0.5).all() and (big.weights[:, :, ctx:] == 1.0).all()
+
+    # committed at the end, and kept by an eviction whose weights name 300 slots
+    path = torch.tensor([[0, 5, 6]], dtype=torch.int32).cuda()
+    G.glance_cache_commit_path(big, c.k_new.cuda(), c.v_new.cuda(), torch.tensor([2], dtype=torch.int32).cuda(), path)
+    assert big.ctx_lens.item() == ctx + 3
+    rng = np.random.default_rng(0)
+    slots = np.sort(rng.choice(np.arange(10, ctx - 20), size=(hkv, 300)), axis=1)
+    big.weights.zero_()
+    want = []
+    for g in range(hkv):
+        mine = np.unique(slots[g])
+        big.weights[0, g, torch.tensor(mine).cuda()] = torch.rand(len(mine)).cuda() + 1
+        want.append(list(range(8)) + mine.tolist() + list(range(ctx + 3 - 12, ctx + 3)))
+    budget = min(len(x) for x in want)
+    want = [x if len(x) == budget else None for x in want]
+    to = G.new_cache(1, hkv, budget, d, dtype=DT[dtype], fmt=fmt, weights=True)
+    kept = G.glance_cache_evict(big, to, budget, 8, 12)
+    torch.cuda.synchronize()
+    for g in range(hkv):
+        if want[g] is not None:
+            assert kept[0, g].cpu().tolist() == want[g]
+        for t, s in ((to.k, big.k), (to.v, big.v), (to.k_scale, big.k_scale), (to.v_scale, big.v_scale)):
+            if t is not None:
+                assert torch.equal(t[0, g], torch.stack([s[0, g, j] for j in kept[0, g].tolist()]))
+    if fmt == "dense":
+        assert torch.equal(to.k[0, :, -3:].cpu(), c.k_new[0, [0, 5, 6]].transpose(0, 1))
 
 
 # ------------------------------------------------------------- together
