@@ -123,7 +123,7 @@ KERNEL_KEYS = {"draft": "attn_bf16<128, false", "verify": "attn_bf16<128, true",
                "accept": "argmax_partial<true, false>", "tree_scan": "tree_scan<true>",
                "tree_rank": "tree_rank<true>", "tree_enum": "tree_enum",
                "sample": "sample_partial<true>"}
-KERNEL_SRC = {"draft": "attn_bf16.hip", "verify": "attn_bf16.hip", "accept": "accept.hip",
+KERNEL_SRC = {"draft": "attn_bf16.h", "verify": "attn_bf16.h", "accept": "accept.hip",
               "tree_scan": "tree.hip", "tree_rank": "tree.hip", "tree_enum": "tree.hip",
               "sample": "accept.hip"}
 
@@ -605,7 +605,7 @@ def roofline(w, k_us, c_us, work, per_kernel):
     # the dominant step as the whole call (attention + its merge pass)
     roof["frac_with_merge"] = round(roof["frac"] * k_us[dom] / c_us[dom], 4)
     src = os.path.join(ROOT, "paper_2609_00355_amd", "csrc",
-                       "accept.hip" if dom == "accept" else "attn_bf16.hip" if w.dtype == "bf16" else "attn_f32.hip")
+                       "accept.hip" if dom == "accept" else "attn_bf16.h" if w.dtype == "bf16" else "attn_f32.h")
     roof["traffic"] = load_traffic(dom, src, w.name)
     roof["kernel"] = per_kernel[dom]["kernel"]
     roof["launch_us"] = round(k_us[dom], 2)
