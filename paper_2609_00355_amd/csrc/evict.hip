@@ -6,10 +6,8 @@
 // NaN counts as larger than every number.
 //
 // Selection, by a workgroup of a (sequence, KV head): the least kept weight by
-// radix selection on order-preserving keys, then the kept slots in order by prefix
-// sums.  The first count takes 11 bits (sign, exponent and two of the fraction),
-// which leaves few enough keys to go on with in LDS.  Bound by latency: one read
-// of the weights and about fifteen barriers.  Then the kept rows of K, V, scales
+// counts of order-preserving keys, then the kept slots in order by prefix sums.
+// Bound by latency: one read of the weights and about a dozen barriers.  Then the kept rows of K, V, scales
 // and weights are copied, 16 bytes a lane, bound by memory.
 //
 // Where LDS holds every key of the cache, the workgroups of a head (as many as
@@ -25,22 +23,24 @@ namespace glance {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kChunk = 4 * kSelectThreads;  // slots the workgroup reads with one load a lane
 constexpr int kChunks = 4;                  // chunks in flight
-constexpr int kBins = 2048;
+constexpr int kBinBits = 11, kBins = 1 << kBinBits;
 constexpr int kHeld = 32768;                // keys held in LDS: those of the first slots
 constexpr int kListed = 4096;               // ... and those still in question
+constexpr unsigned kRanked = 128;           // ... when they are ranked directly
 
-// Unsigned order of weights: -0 and +0 are equal, every NaN is the largest.  No
-// key is 0, which stands for a slot that is not up for selection.
-__device__ __forceinline__ unsigned order_key(float w) {
+// Keys: the unsigned order of weights, -0 and +0 equal and every NaN the largest,
+// between one for slots there are not and one for slots kept whatever they weigh.
+constexpr unsigned kNever = 0, kAlways = 0xffffffffu;
+__device__ __forceinline__ unsigned order_key(unsigned bits) {
+  const float w = __builtin_bit_cast(float, bits);
   const int u = __builtin_bit_cast(int, w + 0.f);  // -0 becomes +0
   const unsigned k = (unsigned)(u ^ (u >> 31 | (int)0x80000000));
-  return w != w ? 0xffffffffu : k;
+  return w != w ? kAlways - 1 : k - 1;
 }
 
 __device__ __forceinline__ int clamp_len(int len, int cap) { return len < 0 ? 0 : (len > cap ? cap : len); }
@@ -53,6 +53,25 @@ __device__ __forceinline__ int row_incl_sum(int v) {
   v += plan_dpp<0x114, 0xf, 0>(v);  // row_shr:4
   v += plan_dpp<0x118, 0xf, 0>(v);  // row_shr:8
   return v;
+}
+// Largest value of each row of 16 lanes, and of the wave, in every lane.
+__device__ __forceinline__ unsigned row_umax(unsigned v) {
+  v = max(v, (unsigned)plan_dpp<0xb1, 0xf, 0>((int)v));   // quad_perm [1,0,3,2]
+  v = max(v, (unsigned)plan_dpp<0x4e, 0xf, 0>((int)v));   // quad_perm [2,3,0,1]
+  v = max(v, (unsigned)plan_dpp<0x141, 0xf, 0>((int)v));  // row_half_mirror
+  return max(v, (unsigned)plan_dpp<0x140, 0xf, 0>((int)v));  // row_mirror
+}
+__device__ __forceinline__ unsigned wave_umax(unsigned v) {
+  v = row_umax(v);
+  v = max(v, (unsigned)plan_dpp<0x142, 0xa, 0>((int)v));  // row_bcast:15
+  v = max(v, (unsigned)plan_dpp<0x143, 0xc, 0>((int)v));  // row_bcast:31
+  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+// Sum of each aligned run of eight lanes, in all of them (whole runs active).
+__device__ __forceinline__ int eight_sum(int v) {
+  v += plan_dpp<0xb1, 0xf, 0>(v);         // quad_perm [1,0,3,2]
+  v += plan_dpp<0x4e, 0xf, 0>(v);         // quad_perm [2,3,0,1]
+  return v + plan_dpp<0x141, 0xf, 0>(v);  // row_half_mirror
 }
 static_assert(kSelectWaves == 16, "a row of lanes holds the waves' counts");
 
@@ -106,7 +125,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   __shared__ u32x4 s_keys[kHeld / 4];
   __shared__ unsigned s_hist[kBins];
   __shared__ unsigned s_list[kListed];
-  __shared__ unsigned s_sum[kSelectWaves], s_found[3], s_n;
+  __shared__ unsigned s_sum[kSelectWaves], s_found[3], s_rank[3], s_n;
+  __shared__ uint2 s_range[kSelectWaves];
   __shared__ int2 s_count[2][kSelectWaves];
   const int head = blockIdx.x, b = head / p.hkv;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -130,31 +150,45 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   const int lo = p.n_sinks, hi = len - p.n_recent;  // slots that have to earn their place
   unsigned need = (unsigned)(p.budget - p.n_sinks - p.n_recent);
 
-  // The keys of slots j0 + kChunk c + 4 tid + i, 0 for those not up for
-  // selection.  A thread's slots are its own in every pass, so it finds its
-  // keys in LDS without a barrier; only longer sequences' are read again.
+  // The keys of slots j0 + kChunk c + 4 tid + i.  A thread's slots are its own in
+  // every pass, so it finds its keys in LDS without a barrier; only longer
+  // sequences' are read again.
   auto fetch = [&](int j0, u32x4 (&k)[kChunks]) __attribute__((always_inline)) {
-    typedef f32x4 __attribute__((aligned(4))) loose;
-    f32x4 v[kChunks];
+    typedef u32x4 __attribute__((aligned(4))) loose;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       const int j = j0 + kChunk * c + 4 * tid;
-      v[c] = f32x4{};
-      if (len >= 4) v[c] = *reinterpret_cast<const loose*>(w + min(j, len - 4));
+      k[c] = u32x4{};
+      if (len >= 4) k[c] = *reinterpret_cast<const loose*>(w + min(j, len - 4));
     }
+    unsigned top = 0;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       const int j = j0 + kChunk * c + 4 * tid;
       if (j > len - 4) {  // the last slots, one by one
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[c][i] = w[min(j + i, len - 1)];
+        for (int i = 0; i < 4; ++i) k[c][i] = __builtin_bit_cast(unsigned, w[min(j + i, len - 1)]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) k[c][i] = order_key(v[c][i]);
-      const int first = j0 + kChunk * c;
+      for (int i = 0; i < 4; ++i) top = max(top, k[c][i]);
+    }
+    // (weights are sums of exponentials: all of a wave's are mostly 0 or more)
+    if (__builtin_amdgcn_ballot_w64(top > 0x7f800000u) == 0) {
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) k[c] += 0x7fffffffu;  // order_key() of these
+    } else {
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[c][i] = order_key(k[c][i]);
+    }
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      const int first = j0 + kChunk * c, j = first + 4 * tid;
       if (first < lo || first + kChunk > hi) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) k[c][i] = j + i >= lo && j + i < hi ? k[c][i] : 0u;
+        for (int i = 0; i < 4; ++i)
+          k[c][i] = j + i >= lo && j + i < hi ? k[c][i] : j + i < len ? kAlways : kNever;
       }
       if (j0 < kHeld) s_keys[j / 4] = k[c];
     }
@@ -166,78 +200,140 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
   };
   static_assert(kHeld % (kChunks * kChunk) == 0, "a read is held in whole or not at all");
 
-  // The need-th largest key, its bits from the top, 11, 11 and 10 at a time: a
-  // count of the keys by their next bits, among those that agree with the bits
-  // found so far.  Once these fit they are copied into a list of their own.
-  unsigned prefix = 0, equal = 0;
-  bool listed = false;
-  int n_list = 0;
+  // The need-th largest key, by counts in kBins bins: of the keys from the least
+  // to the largest, then of those in the bin where the count from the top reaches
+  // `need`, until a bin is one key.  Bins of the keys' own range, not of fixed
+  // bits, spread them over more bins, so that fewer lanes add to one at a time,
+  // and leave few keys in each.  Bin 0 is never counted: it has what the others
+  // leave (weights of 0, often many, are there).  Keys of the last bin are listed
+  // once they fit, and ranked one against the other once they are few.
+  //
+  // Four waves share a SIMD, so an instruction a key costs 256 cycles here.
+  unsigned base = kAlways, equal = 0;
   if (need > 0) {
-    for (int level = 0; level < 3; ++level) {
-      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0;
-      const int bins = level == 2 ? 1024 : kBins;
-      const unsigned known = level == 0 ? 0u : ~0u << (level == 1 ? 21 : 10);  // bits found so far
-      for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
-      if (tid == 0) s_n = 0;
-      __syncthreads();
-      auto count = [&](unsigned k) __attribute__((always_inline)) {
-        if ((k & known) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
-      };
-      if (listed) {
-        for (int i = tid; i < n_list; i += kSelectThreads) count(s_list[i]);
-      } else {
-        for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
-          u32x4 k[kChunks];
-          if (level == 0) {
-            fetch(j0, k);
+    unsigned most = 0, least = 0;  // largest key plus 1, least key's complement plus 1 (kNever, kAlways: 1, 0 and 0, 1)
+    for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
+      u32x4 k[kChunks];
+      fetch(j0, k);
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c)
+      for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (k[c][i] != 0) atomicAdd(&s_hist[k[c][i] >> 21], 1u);
-          } else {
-            read(j0, k);
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) count(k[c][i]);
-          }
+        for (int i = 0; i < 4; ++i) {
+          most = max(most, k[c][i] + 1);
+          least = max(least, 0u - k[c][i]);
         }
+    }
+    for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
+    if (tid == 0) s_n = 0;
+    most = wave_umax(most);
+    least = wave_umax(least);
+    if (lane == 0) s_range[wave] = make_uint2(most, least);
+    __syncthreads();
+    const uint2 range = s_range[lane & 15];
+    most = (unsigned)__builtin_amdgcn_readfirstlane((int)row_umax(range.x)) - 1;
+    base = 0u - (unsigned)__builtin_amdgcn_readfirstlane((int)row_umax(range.y));
+    unsigned span = most - base;   // the keys in question: base .. base + span
+    equal = (unsigned)(hi - lo);   // how many they are
+    bool listed = false;
+    for (bool first = true;; first = false) {
+      const int shift = span >> kBinBits ? 32 - kBinBits - __builtin_clz(span) : 0;
+      const unsigned step = 1u << shift;
+      if (!first) {
+        for (int i = tid; i < kBins; i += kSelectThreads) s_hist[i] = 0;
+        __syncthreads();
       }
-      __syncthreads();
-      // the bin in which the count from the top reaches `need`: every wave sums
-      // its 128 bins, and the one with the crossing finds it
-      const unsigned hi_bin = s_hist[kBins - 1 - 128 * wave - 2 * lane], lo_bin = s_hist[kBins - 2 - 128 * wave - 2 * lane];
-      const unsigned incl = (unsigned)wave_incl_sum((int)(hi_bin + lo_bin));
-      if (lane == 63) s_sum[wave] = incl;
-      __syncthreads();
-      const int sum = (int)s_sum[lane & 15], sums = row_incl_sum(sum);
-      const unsigned before = (unsigned)__builtin_amdgcn_readlane(sums - sum, wave);
-      const unsigned at_hi = before + incl - hi_bin - lo_bin, at_lo = at_hi + hi_bin;
-      const bool in_hi = at_hi < need && need <= at_lo, in_lo = at_lo < need && need <= at_lo + lo_bin;
-      if (in_hi || in_lo) {  // one lane of the workgroup
-        s_found[0] = (unsigned)(kBins - 1 - 128 * wave - 2 * lane - (in_lo ? 1 : 0));
-        s_found[1] = need - (in_lo ? at_lo : at_hi);
-        s_found[2] = in_lo ? lo_bin : hi_bin;
-      }
-      __syncthreads();
-      prefix |= s_found[0] << shift;
-      need = s_found[1];
-      equal = s_found[2];
-      if (!listed && level < 2 && equal <= kListed) {
-        const unsigned mask = ~0u << shift;
+      // of the keys from bin 1 on (all others, kNever and kAlways too, wrap past them)
+      auto count = [&](unsigned k) __attribute__((always_inline)) {
+        const unsigned d = k - (base + step);
+        if (d <= span - step) atomicAdd(&s_hist[1 + (d >> shift)], 1u);
+      };
+      if (span == 0) {
+      } else if (listed) {
+        for (int i = tid; i < (int)equal; i += kSelectThreads) count(s_list[i]);
+      } else {
         for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
           u32x4 k[kChunks];
           read(j0, k);
 #pragma unroll
           for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if ((k[c][i] & mask) == prefix) s_list[atomicAdd(&s_n, 1u)] = k[c][i];
+            for (int i = 0; i < 4; ++i) count(k[c][i]);
         }
-        n_list = (int)equal;
+      }
+      __syncthreads();
+      // the bin in which the count from the top reaches `need`: every wave sums
+      // its 128 bins, and the one with the crossing finds it
+      const int bin = kBins - 2 - 128 * wave - 2 * lane;  // and the one above it
+      const unsigned hi_bin = s_hist[bin + 1], lo_count = s_hist[bin];
+      const unsigned incl = (unsigned)wave_incl_sum((int)(hi_bin + lo_count));
+      if (lane == 63) s_sum[wave] = incl;
+      __syncthreads();
+      const int sum = (int)s_sum[lane & 15], sums = row_incl_sum(sum);
+      const unsigned before = (unsigned)__builtin_amdgcn_readlane(sums - sum, wave);
+      const unsigned at_hi = before + incl - hi_bin - lo_count, at_lo = at_hi + hi_bin;
+      const unsigned lo_bin = bin == 0 ? equal - at_lo : lo_count;
+      const bool in_hi = at_hi < need && need <= at_lo, in_lo = at_lo < need && need <= at_lo + lo_bin;
+      if (in_hi || in_lo) {  // one lane of the workgroup
+        s_found[0] = (unsigned)(in_lo ? bin : bin + 1);
+        s_found[1] = need - (in_lo ? at_lo : at_hi);
+        s_found[2] = in_lo ? lo_bin : hi_bin;
+      }
+      __syncthreads();
+      base += (unsigned)__builtin_amdgcn_readfirstlane((int)s_found[0]) << shift;
+      need = (unsigned)__builtin_amdgcn_readfirstlane((int)s_found[1]);
+      equal = (unsigned)__builtin_amdgcn_readfirstlane((int)s_found[2]);
+      span = min(step - 1, most - base);
+      if (shift == 0) break;
+      if (!listed && equal <= kListed) {
+        for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
+          u32x4 k[kChunks];
+          read(j0, k);
+          unsigned long long in[4 * kChunks];
+          int n = 0;
+#pragma unroll
+          for (int x = 0; x < 4 * kChunks; ++x) {
+            in[x] = __builtin_amdgcn_ballot_w64(k[x / 4][x % 4] - base <= span);
+            n += __popcll(in[x]);
+          }
+          if (n == 0) continue;
+          int at = 0;
+          if (lane == 0) at = (int)atomicAdd(&s_n, (unsigned)n);
+          at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+          for (int x = 0; x < 4 * kChunks; ++x) {
+            if (in[x] == 0) continue;
+            if (in[x] >> lane & 1u)
+              s_list[at + __builtin_amdgcn_mbcnt_hi((unsigned)(in[x] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)in[x], 0))] = k[x / 4][x % 4];
+            at += __popcll(in[x]);
+          }
+        }
         listed = true;
         __syncthreads();
+        if (equal <= kRanked) {
+          // eight lanes a key, each with an eighth of the others
+          const int mine = tid / 8;
+          if (mine < (int)equal) {
+            const unsigned key = s_list[mine];
+            int above = 0, same = 0;
+            for (int i = tid % 8; i < (int)equal; i += 8) {
+              const unsigned k = s_list[i];
+              above += k > key ? 1 : 0;
+              same += k == key ? 1 : 0;
+            }
+            above = eight_sum(above);
+            same = eight_sum(same);
+            if (above < (int)need && (int)need <= above + same) {  // one key, perhaps of several slots
+              s_rank[0] = key;
+              s_rank[1] = need - above;
+              s_rank[2] = same;
+            }
+          }
+          __syncthreads();
+          base = s_rank[0];
+          need = s_rank[1];
+          equal = s_rank[2];
+          break;
+        }
       }
     }
   }
@@ -272,45 +368,41 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
 #pragma unroll
       for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) add(mine, c, k[c][i] == prefix ? 1 : 0);
+        for (int i = 0; i < 4; ++i) add(mine, c, k[c][i] == base ? 1 : 0);
       const int2 at = scan(mine, total);
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
         int rank = ties + half(at, c);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (k[c][i] == prefix && rank++ >= (int)need) k[c][i] = 1;  // below every key
+          if (k[c][i] == base && rank++ >= (int)need) k[c][i] = kNever;
         ties += half(total, c);
       }
     }
-    unsigned keep[kChunks];
     int2 mine = make_int2(0, 0);
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
-      const int j = j0 + kChunk * c + 4 * tid;
-      keep[c] = 0;
+      int n = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool mid = k[c][i] != 0;
-        keep[c] |= (mid ? !none && k[c][i] >= prefix : j + i < len) ? 1u << i : 0u;
-      }
-      add(mine, c, __popc(keep[c]));
+      for (int i = 0; i < 4; ++i) n += k[c][i] >= base ? 1 : 0;
+      add(mine, c, n);
     }
     const int2 at = scan(mine, total);
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       const int j = j0 + kChunk * c + 4 * tid;
       int place = out + half(at, c);
+      out += half(total, c);
+      if (GATHER && (place >= r1 || place + 4 <= r0)) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (keep[c] >> i & 1u) {
+        if (k[c][i] >= base) {
           // (a place is at most its slot, and the barrier in scan() lies behind
           // every read of the keys up to this chunk's: none is overwritten unread)
           if (!GATHER) kept[place] = j + i;
           else if (place >= r0 && place < r1) s_kept[place - r0] = j + i;
           ++place;
         }
-      out += half(total, c);
     }
   }
   if (GATHER) {
