@@ -163,8 +163,9 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
   TileMap tm = {};
   if (WIN) tm = tile_map<64>(p, ctx);
   const int ct = WIN ? tm.n : (ctx + 63) / 64;  // context tiles; tile ct holds the new keys
-  // first key of context tile j
-  auto key_of = [&](int j) __attribute__((always_inline)) { return 64 * (WIN ? tm.at(j) : j); };
+  // tile of the sequence that context tile j is, and its first key
+  auto tile_of = [&](int j) __attribute__((always_inline)) { return WIN ? tm.at(j) : j; };
+  auto key_of = [&](int j) __attribute__((always_inline)) { return 64 * tile_of(j); };
   const int n_tiles = pc.n_tiles;
   const int tb = pc.t_begin;
   const bool has_new = tb + n_tiles - 1 == ct;
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     const int key0 = key_of(j);
     if (!KV4 && j < ct && key0 + 64 <= ctx && (!WIN || key0 >= tm.lo || key0 + 64 <= p.n_sinks)) {
       // full context tile: SGPR base + fixed lane offsets
-      const char* base = gfull + (((size_t)b * p.hkv + g) * p.cap + (size_t)key0) * RB;
+      const char* base = gfull + (((size_t)b * p.hkv + g) * p.cap + 64 * (size_t)tile_of(j)) * RB;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         dma16(base + i * kStep * RB, (unsigned)(lrow * RB) + lchunk, lds + stride * i * 1024);
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     unsigned rstride;
     int nvalid;
     if (!KV4 && j < ct) {  // (a 4-bit cache's tiles do not come here)
-      base = gfull + (((size_t)b * p.hkv + g) * p.cap + (size_t)key0) * RB;
+      base = gfull + (((size_t)b * p.hkv + g) * p.cap + 64 * (size_t)tile_of(j)) * RB;
       rstride = RB;
       nvalid = WIN ? min(64, ctx - key0) : ctx - key0;
     } else {
@@ -288,7 +289,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     const int j = tb + min(t, n_tiles - 1);
     const bool is_ctx = j < ct;
     const int key0 = key_of(j);
-    const char* base = is_ctx ? (v_side ? vc : kc) + (((size_t)b * p.hkv + g) * p.cap + (size_t)key0) * RB
+    const char* base = is_ctx ? (v_side ? vc : kc) + (((size_t)b * p.hkv + g) * p.cap + 64 * (size_t)tile_of(j)) * RB
                               : (v_side ? vn : kn) + ((size_t)b * p.n * p.hkv + g) * RB;
     const unsigned rstride = is_ctx ? RB : (unsigned)p.hkv * RB;
     const int nvalid = is_ctx ? min(64, ctx - key0) : p.n;
@@ -844,6 +845,10 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
       xphase(SK_, YES{}, YES{}, STAGED || wave >= 4 ? t : -1);
     };
     int t = 1;
+    // Where the steps' code begins within a 64-byte line matters with seven
+    // computing waves: 16 ragged verifies of up to 32768 keys in a round took
+    // 468 us with the first step's barrier at byte 40, 477 at 52, 475 at 48.
+    if constexpr (D == 128 && TREE && WIDE) asm volatile(".p2align 6\n\t.rept 14\n\ts_nop 0\n\t.endr");
     while (t < n_tiles) {
       step(t, I1{});
       if (++t >= n_tiles) break;
