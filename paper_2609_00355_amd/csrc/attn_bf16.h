@@ -33,6 +33,23 @@
 // accordingly (no shuffles), and the row of a lane never changes, so the
 // running max and sum are per lane (lanes l and l+32 share a row).
 //
+// A cache read in part (WIN).  The context tiles that some row sees, those of the
+// first keys and those from row 0's window on, are numbered end to end and cut
+// into pieces; rows of them that no row sees are never read (the nearest seen row
+// is, and masked).  A cache in 4 bits (KV4) comes as codes and scales by way of
+// registers; the waves without rows store its bf16 values, which are exact, into
+// the stages that a dense cache's DMA would fill, so the matrix phases are the same.
+//
+// Measured: one row a sequence, 28/4 heads of 128, 16 sequences, window 4096 and 4
+// first keys: 31.6 us, 26.3 for its bytes at the rate of a large copy (bound by
+// memory).  64 rows, the same window, 64 first keys, 4 sequences: 30.5, 12.4 for its products at the
+// rate of a large matrix product: start-up 6, eight tiles of 1.7, the merge 6.
+// 4-bit caches: 16 rows over 4 x 16384 keys 27.5 (a dense cache: 36 to 40), 12.2 for
+// its products: 16 tiles of 1.0, bound by the vector instructions of the softmax and
+// by LDS, of which the operands take 1300 and the conversion's stores 400 cycles of
+// a tile's 2150; 64 rows over 16 ragged caches 284, 211 for its products: the one
+// converting wave takes 3450 cycles a tile, which the computing waves need as well.
+//
 // Merge.  A piece that is its sequence's only one writes the output and LSE.
 // Otherwise each piece writes its normalised output in fp16 (in the MFMA
 // register layout, four values per lane per store, each row scaled by a power

