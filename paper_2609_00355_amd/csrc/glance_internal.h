@@ -37,7 +37,7 @@ struct AttnParams {
   int nsplit;     // split slots per (sequence, KV head) = ceil(cap / split_keys), >= 1 (fp32 kernel)
   int split_keys; // context keys per split, a multiple of 16 (fp32 kernel)
   float scale_log2;  // sm_scale * log2(e)
-  // bf16 kernel: pieces planned on the device from ctx_lens (see attn_bf16.hip)
+  // bf16 kernel: pieces planned on the device from ctx_lens (see attn_bf16.h)
   int slots_per_g;  // piece slots per KV head (>= batch)
   int min_tiles;    // smallest piece, in 64-key tiles
   int tiles_rg;     // 32-row tiles per row group (= computing waves, 1..7)
