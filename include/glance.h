@@ -356,8 +356,8 @@ glance_status glance_build_tree(int32_t batch, int32_t horizon, int32_t vocab, i
  *               [0, capacity] where read)
  *   weights     device [batch][Hkv][capacity] float32, or NULL where no call
  *               that needs them is made
- * k, v and the scales are 16-byte aligned.  Slots at or past ctx_lens are never
- * read, except that rows committed or weighed go there.
+ * k, v and the scales are 16-byte aligned.  What slots at or past ctx_lens hold
+ * does not matter; rows committed or weighed go there.
  *
  * 4-bit values: 32 consecutive dims of a key (or value) share a power of two
  * 2^e and each is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e (codes
