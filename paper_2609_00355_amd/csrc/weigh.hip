@@ -25,9 +25,10 @@
 // exact and summed in fp32 by the matrix unit.
 //
 // Bound by the read of the keys where the rows are few: about 10 path nodes of 7
-// heads over 4 caches of 16384 bf16 keys and 4 heads of 128 (67 MB) take 22.1 us,
+// heads over 4 caches of 16384 bf16 keys and 4 heads of 128 (67 MB) take 21.0 us,
 // 13.8 at the rate of a large copy, of which 4 are the chain of loads from the
-// lengths to the first key (asked for only once the path was known: 24.7).  With
+// lengths to the first key (asked for only once the path was known, and with a
+// dozen spilled addresses: 24.7).  With
 // more rows by vector instructions, an exponential, a multiply-add and an addition
 // a score: 16 rows of 7 heads over 16 ragged caches of 2048 to 32768 4-bit keys
 // take 47 us, 26 at the rate of a large matrix product.
@@ -236,37 +237,39 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
     // a thread in flight at once, and behind the first of these (loads arrive in
     // order) the first step's keys, where they are not there yet.
     static_assert(kRows <= kThreads, "a row a thread");
+    int t = tid;
+    asm volatile("" : "+v"(t));  // addresses made from it here are not kept, spilled, for another turn
     float lse = __builtin_inff();
     {
-      const int i = min(r0 + tid, max(total - 1, 0)) / p.group;
+      const int i = min(r0 + t, max(total - 1, 0)) / p.group;
       const int node_i = path ? __shfl(node, i) : i;
-      const int at = (b * p.n + node_i) * p.hq + g * p.group + (r0 + tid - i * p.group);
-      if (tid < n_rows) lse = p.lse[at];
-      if (tid < kRows) {
-        sPlace[tid] = i;
-        sRow[tid] = tid < n_rows ? at : -1;
+      const int at = (b * p.n + node_i) * p.hq + g * p.group + (r0 + t - i * p.group);
+      if (t < n_rows) lse = p.lse[at];
+      if (t < kRows) {
+        sPlace[t] = i;
+        sRow[t] = t < n_rows ? at : -1;
       }
-      if (tid == 0) sTicket = kWeighWaves;
+      if (t == 0) sTicket = kWeighWaves;
     }
     __syncthreads();
     int s = wave;  // the first step; the others by ticket
     for (int u0 = 0; u0 < padded * CH || u0 == 0; u0 += kBatch * kThreads) {
+      int row[kBatch];
       u32x4 v[kBatch];
 #pragma unroll
-      for (int x = 0; x < kBatch; ++x) {
-        const int u = u0 + x * kThreads + tid, r = u / CH, c = u % CH;
-        const int row = r < padded ? sRow[r] : -1;
-        v[x] = u32x4{};
-        if (row >= 0) v[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (size_t)row * RB + 16 * c);
-      }
+      for (int x = 0; x < kBatch; ++x) row[x] = sRow[min((u0 + x * kThreads + t) / CH, kRows - 1)];
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x)  // (for padding rows any query)
+        v[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.q) + (size_t)max(row[x], 0) * RB + 16 * (t % CH));
       if (u0 == 0 && s < n_steps && !(r0 == 0 && first_held)) load(step_at(s));
 #pragma unroll
       for (int x = 0; x < kBatch; ++x) {
-        const int u = u0 + x * kThreads + tid, r = u / CH, c = u % CH;
-        if (r < padded) *reinterpret_cast<u32x4*>(sQ + r * LB + 16 * c) = v[x];
+        const int r = (u0 + x * kThreads + t) / CH;
+        if (r < padded) *reinterpret_cast<u32x4*>(sQ + r * LB + 16 * (t % CH)) = row[x] >= 0 ? v[x] : u32x4{};
       }
     }
-    if (tid < kRows) sOff[tid] = -lse * kLog2e;
+    static_assert(kThreads % CH == 0, "a thread's chunk of a query is one and the same");
+    if (t < kRows) sOff[t] = -lse * kLog2e;
     __syncthreads();
     while (s < n_steps) {
       const Step st = step_at(s);
