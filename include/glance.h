@@ -420,8 +420,8 @@ size_t glance_cache_attn_workspace_size(const glance_attn_shape* s, int32_t n_si
  * dense and the other in 4 bits (a prefilled cache goes into 4 bits; a 4-bit
  * one comes back as the values it stands for, exactly).  Slots below
  * min(src length, dst capacity) are written, and dst's lengths set to that;
- * weights stay as they are.  src and dst must not overlap; the two may share
- * ctx_lens.
+ * weights stay as they are.  src and dst must not overlap; their ctx_lens
+ * are one array or apart.
  */
 glance_status glance_cache_convert(const glance_cache* src, const glance_cache* dst, hipStream_t stream);
 
@@ -471,7 +471,7 @@ glance_status glance_cache_weigh(const glance_attn_shape* s, const glance_cache*
  *   budget      1..dst's capacity; n_sinks + n_recent <= budget
  *   dst         K, V, scales and weights of slots below min(length, budget) are
  *               written, the others left as they are; ctx_lens becomes that
- *               minimum (src's may be the same array).  No other buffer may
+ *               minimum (src's is the same array or apart).  No other buffer may
  *               overlap src's.
  *   kept        device [batch][Hkv][budget] int32: the source slot of each kept
  *               one, then -1

@@ -453,10 +453,8 @@ hipError_t launch_evict(const EvictParams& p, hipStream_t s, hipEvent_t ev0, hip
   const long long units = (long long)p.budget * (p.src.row_bytes / 16);
   const dim3 grid((unsigned)((units + kGatherThreads - 1) / kGatherThreads), (unsigned)heads, 2);
   if (ev0) (void)hipEventRecord(ev0, s);
-  // shared lengths: other workgroups of the one launch still read what it writes
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p.src.lens), b = reinterpret_cast<uintptr_t>(p.dst.lens);
-  const bool apart = (a > b ? a - b : b - a) >= (size_t)p.batch * sizeof(int);
-  if (p.src.cap <= kHeld && apart) {
+  // (with shared lengths other workgroups of the one launch would still read what it writes)
+  if (p.src.cap <= kHeld && p.src.lens != p.dst.lens) {
     const int parts = heads < 256 ? 256 / heads : 1;
     hipLaunchKernelGGL(evict_select<true>, dim3((unsigned)heads, (unsigned)parts), dim3(kSelectThreads), 0, s, p);
     const hipError_t e = hipGetLastError();

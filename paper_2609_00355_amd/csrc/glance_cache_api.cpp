@@ -135,6 +135,9 @@ glance_status check_pair(const glance_cache* src, const glance_cache* dst) {
     for (auto& y : b)
       if (overlap(x.ptr, x.bytes, y.ptr, y.bytes))
         return fail(GLANCE_ERR_INVALID_ARG, "src and dst must not overlap");
+  const size_t lens = (size_t)src->batch * sizeof(int32_t);
+  if (src->ctx_lens != dst->ctx_lens && overlap(src->ctx_lens, lens, dst->ctx_lens, lens))
+    return fail(GLANCE_ERR_INVALID_ARG, "src's and dst's ctx_lens must be one array or apart");
   return ok();
 }
 

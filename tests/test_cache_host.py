@@ -175,6 +175,14 @@ def test_evict_refusals(lib, src, dst, kw, code, word):
     assert word in G.glance_last_error()
 
 
+def test_lengths_that_overlap_in_part_are_refused(lib):
+    src, conv, ev = _cache(batch=4), _kv4(16, batch=4, ctx_lens=FAKE + 8), _cache(16, batch=4, ctx_lens=FAKE - 12)
+    assert lib.glance_cache_convert(ctypes.byref(src), ctypes.byref(conv), None) == BAD
+    assert "ctx_lens" in G.glance_last_error()
+    assert lib.glance_cache_evict(ctypes.byref(src), ctypes.byref(ev), 100, 0, 0, FAKE, None) == BAD
+    assert "ctx_lens" in G.glance_last_error()
+
+
 def test_binding_refusals():
     """What the binding turns away before it calls the library, on host tensors."""
     cache = G.new_cache(1, 2, 8, 64, fmt="kv4", weights=True, device="cpu")
