@@ -31,10 +31,11 @@
 //
 // With a window the blocks of 16 keys that some row sees are laid end to end and
 // split alike.  37 rows, 8/2 heads of 64, 3 ragged 4-bit caches of up to 11003
-// keys, of which a window of 2500 and 5 first ones are seen: 18.8 us (15.6 and the
+// keys, of which a window of 2500 and 5 first ones are seen: 18.5 us (15 and the
 // merge), 3.7 at the fp32 matrix rate: 240 workgroups of some 5 us of products and
 // conversions each, start-up, the merge of the waves and the merge of the splits.
-// 16 rows of 4/1 heads of 64, a window of 64 over 256 keys: 6.5, one launch.
+// 16 rows of 4/1 heads of 64, a window of 64 over 256 keys: 6.3, one launch
+// (6.5 with the queries asked for behind the length).
 //
 // Partial results (more than one split): O unnormalised, [row][dim], and
 // (max * scale * log2 e, sum) per row, combined by attn_merge_kernel; a
@@ -90,6 +91,33 @@ __global__ __launch_bounds__(64 * W, 2) void attn_f32(AttnParams p) {
   const int b = bs % p.batch;
   const int s = bs / p.batch;
 
+  // this lane's query rows, dims 16 c + 4 q .. +3 (zeros for padding rows)
+  f32x4 qf[R][KC];
+  int node[R];
+  size_t out_row[R];
+  bool row_ok[R];
+  auto load_rows = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int row = (rg * R + r) * 16 + m16;
+      row_ok[r] = row < p.rows;
+      node[r] = row_ok[r] ? row / p.group : p.n;
+      const int hl = row_ok[r] ? row - node[r] * p.group : 0;
+      out_row[r] = ((size_t)b * p.n + node[r]) * p.hq + (size_t)g * p.group + hl;
+      const float* qp = static_cast<const float*>(p.q) + out_row[r] * D;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) qf[r][c] = row_ok[r] ? *reinterpret_cast<const f32x4*>(qp + kdim(q, c)) : f32x4{};
+    }
+  };
+  // (WIN: the queries and the parents, which do not depend on the length, are
+  // asked for before it is waited for)
+  int par = -1;
+  if (WIN) {
+    load_rows();
+    if (TREE && wave == 0 && lane < p.n) par = p.parents[(size_t)b * p.n + lane];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
   const int ctx = clamp_ctx(p.ctx_lens[b], p.cap);
   TileMap tm = {};
   if (WIN) tm = tile_map<16>(p, ctx);
@@ -106,25 +134,9 @@ __global__ __launch_bounds__(64 * W, 2) void attn_f32(AttnParams p) {
   const int nb_ctx = k_end > k_begin ? (k_end - k_begin + 15) / 16 : 0;
   const int nb = nb_ctx + (has_new ? (p.n + 15) / 16 : 0);
 
-  // this lane's query rows, dims 16 c + 4 q .. +3 (zeros for padding rows)
-  f32x4 qf[R][KC];
-  int node[R];
-  size_t out_row[R];
-  bool row_ok[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int row = (rg * R + r) * 16 + m16;
-    row_ok[r] = row < p.rows;
-    node[r] = row_ok[r] ? row / p.group : p.n;
-    const int hl = row_ok[r] ? row - node[r] * p.group : 0;
-    out_row[r] = ((size_t)b * p.n + node[r]) * p.hq + (size_t)g * p.group + hl;
-    const float* qp = static_cast<const float*>(p.q) + out_row[r] * D;
-#pragma unroll
-    for (int c = 0; c < KC; ++c) qf[r][c] = row_ok[r] ? *reinterpret_cast<const f32x4*>(qp + kdim(q, c)) : f32x4{};
-  }
+  if (!WIN) load_rows();
   const bool tree_words = TREE && (has_new || WIN);
-  int par = -1;
-  if (tree_words && wave == 0 && lane < p.n) par = p.parents[(size_t)b * p.n + lane];
+  if (tree_words && !WIN && wave == 0 && lane < p.n) par = p.parents[(size_t)b * p.n + lane];
 
   // Block j of the split: its first key row, the rows' stride in floats and
   // the number of valid keys.  Rows past the valid ones re-read the last
