@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
     base = 0u - (unsigned)__builtin_amdgcn_readfirstlane((int)row_umax(range.y));
     unsigned span = most - base;   // the keys in question: base .. base + span
     equal = (unsigned)(hi - lo);   // how many they are
-    bool listed = false;
+    int n_list = 0;                // keys listed, 0 before
     for (bool first = true;; first = false) {
       const int shift = span >> kBinBits ? 32 - kBinBits - __builtin_clz(span) : 0;
       const unsigned step = 1u << shift;
@@ -250,8 +250,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
         if (d <= span - step) atomicAdd(&s_hist[1 + (d >> shift)], 1u);
       };
       if (span == 0) {
-      } else if (listed) {
-        for (int i = tid; i < (int)equal; i += kSelectThreads) count(s_list[i]);
+      } else if (n_list) {
+        for (int i = tid; i < n_list; i += kSelectThreads) count(s_list[i]);
       } else {
         for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
           u32x4 k[kChunks];
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
       equal = (unsigned)__builtin_amdgcn_readfirstlane((int)s_found[2]);
       span = min(step - 1, most - base);
       if (shift == 0) break;
-      if (!listed && equal <= kListed) {
+      if (n_list == 0 && equal <= kListed) {
         for (int j0 = 0; j0 < len; j0 += kChunks * kChunk) {
           u32x4 k[kChunks];
           read(j0, k);
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select(EvictParams p) {
             at += __popcll(in[x]);
           }
         }
-        listed = true;
+        n_list = (int)equal;
         __syncthreads();
         if (equal <= kRanked) {
           // eight lanes a key, each with an eighth of the others

@@ -393,6 +393,29 @@ def test_evict_with_every_key_held():
                 assert (to.k[b, h, len(slots):] == 0).all()
 
 
+@pytest.mark.parametrize("close", [100, 1000, 3000, 5000])
+def test_evict_among_close_weights(close):
+    """Weights a few units of the last place apart, within a wide range of others: every level of the selection counts."""
+    cap = 6000
+    rng = np.random.default_rng(close)
+    w = np.exp(3 * rng.normal(size=(2, 2, cap))).astype(np.float32) * 1e-3
+    w[:, :, :50] = 0.0
+    for h in range(4):
+        ulps = 37 * np.arange(close) + rng.integers(0, 3, size=close)
+        at = rng.permutation(cap)[:close]
+        w.reshape(4, cap)[h, at] = (np.float32(1.0).view(np.int32) + ulps.astype(np.int32)).view(np.float32)
+    k = torch.arange(cap, dtype=torch.float32).reshape(1, 1, -1, 1).expand(2, 2, -1, 64).contiguous().cuda()
+    src = G.ContextCache(k, k.clone(), torch.tensor([cap, cap - 7], dtype=torch.int32).cuda(), weights=torch.tensor(w).cuda())
+    for budget in (1, close // 3, close // 2 + 41, close, 2500):
+        to = G.new_cache(2, 2, budget, 64, dtype=torch.float32, weights=True)
+        kept = G.glance_cache_evict(src, to, budget, 0, 0)
+        want = OC.evict([cap, cap - 7], w, budget, 0, 0)
+        for b in range(2):
+            for h in range(2):
+                assert kept[b, h].cpu().tolist() == want[b][h], (budget, b, h)
+                assert to.v[b, h, :, 5].cpu().tolist() == [float(x) for x in want[b][h]]
+
+
 def test_evict_with_shared_lengths():
     c = Case("bf16", "dense", 64, 1, 2, 2, [200, 30], seed=1, weights=True)
     to = G.new_cache(2, 2, 64, 64, weights=True)
