@@ -607,9 +607,10 @@ def test_on_another_stream():
     torch.cuda.synchronize()
     s = torch.cuda.Stream()
     q, kn, vn, par = c.q.cuda(), c.k_new.cuda(), c.v_new.cuda(), c.parents.cuda()
-    torch.cuda.synchronize()
+    into = torch.zeros_like(c.cache.weights)
+    torch.cuda.synchronize()  # what the current stream wrote, `into` too, is there before the other one starts
     out, lse = G.glance_cache_tree_verify_attn(q, c.cache, kn, vn, par, 2, 100, stream=s)
-    w = G.glance_cache_weigh(q, c.cache, lse, n_sinks=2, window=100, weights_out=torch.zeros_like(c.cache.weights), stream=s)
+    w = G.glance_cache_weigh(q, c.cache, lse, n_sinks=2, window=100, weights_out=into, stream=s)
     s.synchronize()
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     assert w.sum() > 0
