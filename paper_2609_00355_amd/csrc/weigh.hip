@@ -25,13 +25,13 @@
 // exact and summed in fp32 by the matrix unit.
 //
 // Bound by the read of the keys where the rows are few: about 10 path nodes of 7
-// heads over 4 caches of 16384 bf16 keys and 4 heads of 128 (67 MB) take 21.0 us,
+// heads over 4 caches of 16384 bf16 keys and 4 heads of 128 (67 MB) take 21.5 us,
 // 13.8 at the rate of a large copy, of which 4 are the chain of loads from the
 // lengths to the first key (asked for only once the path was known, and with a
 // dozen spilled addresses: 24.7).  With
 // more rows by vector instructions, an exponential, a multiply-add and an addition
 // a score: 16 rows of 7 heads over 16 ragged caches of 2048 to 32768 4-bit keys
-// take 47 us, 26 at the rate of a large matrix product.
+// take 47 to 50 us, 26 at the rate of a large matrix product.
 #include "glance_internal.h"
 
 #include <type_traits>
@@ -138,6 +138,7 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
   __shared__ __attribute__((aligned(16))) int sPlace[kRows];  // the row's place: position ctx + place
   __shared__ int sRow[kRows];                                 // its query, -1 for padding rows
   __shared__ int sTicket;
+  __shared__ float sPart[64 * kWeighWaves];  // sums of a step's parts
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -163,6 +164,13 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
     int key0, end;  // first key and the keys there are
   };
   const int n_steps = pc.n_tiles * SPT;
+  // fp32, whose products take eight times as long: with fewer steps than half the
+  // waves `parts` waves share one, a part of the row tiles each, and their sums
+  // are added up in order at the end.  64 rows of 12/1 heads over 542 4-bit keys
+  // 61.8 -> 41 us, 36 rows of 28/4 heads over a window of 545 24.6 -> 16.9.  (In
+  // bf16 the registers do not go round: 47.9 -> 50.4 in the largest calls.)
+  const int parts = BF16 || n_steps > 4 ? 1 : n_steps == 1 ? 8 : n_steps == 2 ? 4 : 2;
+  const int part = wave % parts, own_step = wave / parts;
   auto step_at = [&](int s) __attribute__((always_inline)) {
     const int j = pc.t_begin + s / SPT;
     Step o;
@@ -209,7 +217,7 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
     accepted = p.accept_len[b];
     node = lane < most ? p.accept_path[(size_t)b * p.path_stride + lane] : -1;
   }
-  const Step first_step = step_at(min(wave, n_steps - 1));
+  const Step first_step = step_at(min(own_step, n_steps - 1));
   const bool first_held = !first_step.is_new && first_step.key0 < first_step.end;
   load_context(first_held ? first_step : Step{false, 0, 1});
   if (path) {
@@ -252,7 +260,7 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
       if (t == 0) sTicket = kWeighWaves;
     }
     __syncthreads();
-    int s = wave;  // the first step; the others by ticket
+    int s = own_step;  // the first step; the others by ticket
     for (int u0 = 0; u0 < padded * CH || u0 == 0; u0 += kBatch * kThreads) {
       int row[kBatch];
       u32x4 v[kBatch];
@@ -297,14 +305,18 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
       const bool writes = mine < st.end && slot < p.cache.cap && (KB == 2 || h == 0);
       const float keep = r0 > 0 ? 1.f : st.is_new ? 0.f : p.decay;
       const float before = (r0 > 0 || p.decay == 0.f ? out : old)[min(slot, p.cache.cap - 1)];
-      int ticket = 0;
-      if (lane == 0) ticket = atomicAdd(&sTicket, 1);
-      s = __builtin_amdgcn_readfirstlane(ticket);
+      s = n_steps;
+      if (parts == 1) {
+        int ticket = 0;
+        if (lane == 0) ticket = atomicAdd(&sTicket, 1);
+        s = __builtin_amdgcn_readfirstlane(ticket);
+      }
       if (s < n_steps) load(step_at(s));
       if (st.key0 >= st.end) continue;
       float sum[KB][2] = {};
       // a step whose keys every row sees needs no places
       const bool all = !st.is_new && (st.key0 + KEYS <= p.plan.n_sinks || st.key0 >= ctx + rows - p.plan.window);
+      const int rt0 = 32 * part, stride = 32 * parts;  // this wave's row tiles
       auto walk = [&](auto ALL_) __attribute__((always_inline)) {
         constexpr bool ALL = decltype(ALL_)::value;
         int from[KB], to[KB];  // the places of the rows that see the lane's key of each block
@@ -336,9 +348,9 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
           sum[kb][x & 1] += e;
         };
 #pragma unroll
-        for (int i = 0; i < Op::N; ++i) query(0, i);
+        for (int i = 0; i < Op::N; ++i) query(rt0, i);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) offset(0, x);
+        for (int x = 0; x < 4; ++x) offset(rt0, x);
         if constexpr (KB == 2) {
           // Matrix and vector instructions in turn: the products of one block
           // between the exponentials of the other, operands reloaded as soon as
@@ -347,8 +359,8 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
           // rows over 16 ragged caches in 4 bits.)
           constexpr int E = 16 / Op::N;  // exponentials a product
           f32x16 z0 = scores<D, BF16, KV4>(q, k[0]), z1;
-          for (int rt = 0; rt < padded; rt += 32) {
-            const int nt = rt + 32 < padded ? rt + 32 : 0;
+          for (int rt = rt0; rt < padded; rt += stride) {
+            const int nt = rt + stride < padded ? rt + stride : rt0;
 #pragma unroll
             for (int i = 0; i < Op::N; ++i) {
               z1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q.x[i], k[1].x[i], i == 0 ? f32x16{} : z1, 0, 0, 0);
@@ -367,8 +379,8 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
             }
           }
         } else {
-          for (int rt = 0; rt < padded; rt += 32) {
-            const int nt = rt + 32 < padded ? rt + 32 : 0;
+          for (int rt = rt0; rt < padded; rt += stride) {
+            const int nt = rt + stride < padded ? rt + stride : rt0;
             const f32x16 z = scores<D, BF16, KV4>(q, k[0]);
 #pragma unroll
             for (int i = 0; i < Op::N; ++i) query(nt, i);
@@ -379,7 +391,7 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
           }
         }
       };
-      if (padded > 0) {
+      if (rt0 < padded) {
         if (all) walk(std::true_type{});
         else walk(std::false_type{});
       }
@@ -392,7 +404,20 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighParams 
         w = sum[0][0] + sum[0][1];
         w += __shfl_xor(w, 32);
       }
-      if (writes) out[slot] = keep > 0.f ? fmaf(keep, before, w) : w;
+      if (parts > 1) sPart[tid] = w;
+      else if (writes) out[slot] = keep > 0.f ? fmaf(keep, before, w) : w;
+    }
+    if (parts > 1) {
+      __syncthreads();
+      if (part != 0 || own_step >= n_steps) continue;
+      const Step st = step_at(own_step);
+      const int mine = st.key0 + r32 + (KB == 2 ? 32 * h : 0);
+      const int slot = st.is_new ? ctx + mine : mine;
+      if (mine >= st.end || slot >= p.cache.cap || (KB == 1 && h != 0)) continue;
+      float w = sPart[tid];
+      for (int i = 1; i < parts; ++i) w += sPart[tid + 64 * i];
+      const float keep = r0 > 0 ? 1.f : st.is_new ? 0.f : p.decay;
+      out[slot] = keep > 0.f ? fmaf(keep, (r0 > 0 ? out : old)[slot], w) : w;
     }
   }
 }

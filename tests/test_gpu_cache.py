@@ -317,6 +317,23 @@ def test_weigh(fmt, dtype, d, n, hq, hkv, path, n_sinks, window):
         assert torch.equal(c.cache.weights[5, :, :300].cpu(), torch.tensor(got[5, :, :300]))
 
 
+@pytest.mark.parametrize("lens", [[60, 50], [120, 90], [200, 190], [330, 100], [600, 610], [1500, 901]])
+@pytest.mark.parametrize("fmt,dtype", [("dense", "bf16"), ("kv4", "bf16"), ("dense", "f32"), ("kv4", "f32")])
+def test_weigh_in_pieces_of_every_length(fmt, dtype, lens):
+    """Many KV heads, so few workgroups a head: from one step to more steps than waves each."""
+    hkv, n = 64, 40
+    c = Case(dtype, fmt, 64, n, hkv, hkv, lens, seed=lens[0], weights=True)
+    for window, n_sinks in ((0, 0), (70, 3)):
+        lse = torch.tensor(c.want(False, n_sinks, window)[1], dtype=torch.float32)
+        into = torch.zeros_like(c.cache.weights)
+        got = G.glance_cache_weigh(c.q.cuda(), c.cache, lse.cuda(), decay=0.5, n_sinks=n_sinks, window=window, weights_out=into).cpu().numpy()
+        ref = OC.weigh(c.q.double(), c.k64, lse.double(), c.lens, c.weights.double(), 0.5, n_sinks=n_sinks, window=window)
+        for b, ctx in enumerate(lens):
+            bound = _weight_bound(c, lse.numpy(), n, ref[b, :, :ctx])
+            assert (np.abs(got[b, :, :ctx] - ref[b, :, :ctx]) <= bound).all(), (b, window)
+            assert (got[b, :, ctx:] == 0).all()
+
+
 # ------------------------------------------------------------- eviction
 @pytest.mark.parametrize("fmt,dtype,d", [("dense", "bf16", 128), ("dense", "f32", 64), ("kv4", "bf16", 64), ("kv4", "bf16", 128)])
 @pytest.mark.parametrize("budget,n_sinks,n_recent", [(1, 0, 0), (1, 1, 0), (2, 1, 1), (63, 0, 63), (64, 4, 16), (100, 0, 0), (600, 17, 33),
