@@ -603,13 +603,23 @@ def _path_args(accept_len, accept_path, batch):
     return accept_path.shape[1]
 
 
+def _int32(value, name):
+    """ctypes keeps the low 32 bits of a number that is larger: a window of 2^32 would be none."""
+    n = int(value)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits, got {n}")
+    return n
+
+
 def glance_cache_attn_workspace_size(shape, n_sinks=0, window=0):
-    return int(lib().glance_cache_attn_workspace_size(ctypes.byref(shape), int(n_sinks), int(window)))
+    return int(lib().glance_cache_attn_workspace_size(ctypes.byref(shape), _int32(n_sinks, "n_sinks"),
+                                                      _int32(window, "window")))
 
 
 def _cache_attn_args(tree, q, cache, k_new, v_new, parents, n_sinks, window, out, lse, workspace, sm_scale, stream,
                      want_lse):
     torch = _torch()
+    n_sinks, window = _int32(n_sinks, "n_sinks"), _int32(window, "window")
     shape = _cache_query(q, cache, sm_scale)
     _new_rows(k_new, "k_new", q, cache)
     _new_rows(v_new, "v_new", q, cache)
@@ -635,7 +645,7 @@ def _cache_attn_args(tree, q, cache, k_new, v_new, parents, n_sinks, window, out
     if need == 0:
         raise GlanceError(GLANCE_ERR_INVALID_ARG, glance_last_error())
     ws = _workspace(need, q.device, workspace, stream)
-    args = [ctypes.byref(shape), ctypes.byref(view), int(n_sinks), int(window), _ptr(q), _ptr(k_new), _ptr(v_new)]
+    args = [ctypes.byref(shape), ctypes.byref(view), n_sinks, window, _ptr(q), _ptr(k_new), _ptr(v_new)]
     if tree:
         args += [_ptr(parents)]
     args += [_ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)]
@@ -701,6 +711,7 @@ def glance_cache_commit_path(cache, k_new, v_new, accept_len, accept_path, strea
 
 def _weigh_args(q, cache, lse, k_new, accept_len, accept_path, decay, n_sinks, window, weights_out, sm_scale, stream):
     torch = _torch()
+    n_sinks, window = _int32(n_sinks, "n_sinks"), _int32(window, "window")
     shape = _cache_query(q, cache, sm_scale)
     view = _cache_struct(cache, "cache")
     _dev(lse, "lse", torch.float32, 3)
@@ -723,7 +734,7 @@ def _weigh_args(q, cache, lse, k_new, accept_len, accept_path, decay, n_sinks, w
     if tuple(weights_out.shape) != want:
         raise ValueError(f"weights_out must be [batch][Hkv][capacity] = {want}")
     _same_device(q, lse, k_new, accept_len, accept_path, weights_out)
-    args = [ctypes.byref(shape), ctypes.byref(view), int(n_sinks), int(window), _ptr(q), _ptr(lse), _ptr(k_new),
+    args = [ctypes.byref(shape), ctypes.byref(view), n_sinks, window, _ptr(q), _ptr(lse), _ptr(k_new),
             _ptr(accept_len), _ptr(accept_path), stride, float(decay), _ptr(weights_out), _stream(stream)]
     keep = (shape, view, q, lse, k_new, accept_len, accept_path, weights_out) + _cache_tensors(cache)
     return args, weights_out, keep
@@ -743,8 +754,9 @@ def glance_cache_weigh(q, cache, lse, k_new=None, accept_len=None, accept_path=N
 
 def _evict_args(src, dst, budget, n_sinks, n_recent, kept, stream):
     torch = _torch()
+    budget, n_sinks, n_recent = _int32(budget, "budget"), _int32(n_sinks, "n_sinks"), _int32(n_recent, "n_recent")
     a, b = _cache_struct(src, "src"), _cache_struct(dst, "dst")
-    shape = (src.batch, src.n_kv_heads, int(budget))
+    shape = (src.batch, src.n_kv_heads, budget)
     if kept is None:
         if budget < 1:
             raise ValueError(f"budget must be >= 1, got {budget}")
@@ -753,7 +765,7 @@ def _evict_args(src, dst, budget, n_sinks, n_recent, kept, stream):
     if tuple(kept.shape) != shape:
         raise ValueError(f"kept must be [batch][Hkv][budget] = {shape}")
     _same_device(kept)
-    args = [ctypes.byref(a), ctypes.byref(b), int(budget), int(n_sinks), int(n_recent), _ptr(kept), _stream(stream)]
+    args = [ctypes.byref(a), ctypes.byref(b), budget, n_sinks, n_recent, _ptr(kept), _stream(stream)]
     return args, kept, (a, b, kept) + _cache_tensors(src) + _cache_tensors(dst)
 
 

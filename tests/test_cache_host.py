@@ -199,6 +199,24 @@ def test_binding_refusals():
     assert G.new_cache(1, 2, 8, 64, device="cpu").k.dtype == torch.bfloat16
 
 
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32, 2 ** 32 + 8, -2 ** 31 - 1])
+def test_numbers_past_32_bits_are_refused(lib, big):
+    """The library's are 32 bits: cut to them, 2^32 would be no window and 2^32 + 8 one of 8."""
+    cache = G.new_cache(1, 2, 8, 64, weights=True, device="cpu")
+    q, lse = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16), torch.zeros(1, 1, 2)
+    for kw in (dict(n_sinks=big), dict(window=big)):
+        with pytest.raises(ValueError, match=f"{next(iter(kw))} must fit 32 bits"):
+            G.glance_cache_attn_workspace_size(_shape(), **kw)
+        for call in (lambda: G.glance_cache_block_draft_attn(q, cache, q, q, **kw),
+                     lambda: G.prepare_cache_tree_verify_attn(q, cache, q, q, None, **kw),
+                     lambda: G.glance_cache_weigh(q, cache, lse, **kw)):
+            with pytest.raises(ValueError, match="must fit 32 bits"):
+                call()
+    for kw in (dict(budget=big), dict(budget=4, n_sinks=big), dict(budget=4, n_recent=big)):
+        with pytest.raises(ValueError, match="must fit 32 bits"):
+            G.glance_cache_evict(cache, cache, **kw)
+
+
 def test_tensors_of_another_device_are_refused(monkeypatch):
     """The calls run on the current device: a tensor elsewhere would be read by the wrong GPU."""
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
