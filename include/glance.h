@@ -400,7 +400,8 @@ typedef struct {
  * rows, outputs and conventions.  batch, n_kv_heads, head_dim and capacity of
  * the cache must be the shape's, and a dense cache's dtype too; over a 4-bit
  * cache q, k_new, v_new and out are of s->dtype, the keys and values being the
- * exact values of their codes.  The call with n_new = 1 is one decoding step.
+ * exact values of their codes.  Over a dense cache with window 0 they are those
+ * calls, bit for bit.  The call with n_new = 1 is one decoding step.
  *   workspace   >= glance_cache_attn_workspace_size(s, n_sinks, window) bytes
  */
 glance_status glance_cache_block_draft_attn(const glance_attn_shape* s, const glance_cache* cache, int32_t n_sinks,

@@ -639,3 +639,16 @@ def test_same_bits_every_time():
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
     w = [G.glance_cache_weigh(c.q.cuda(), c.cache, a[1], n_sinks=4, window=500, weights_out=torch.zeros_like(c.cache.weights)) for _ in range(2)]
     assert torch.equal(w[0], w[1])
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("dtype,d,n", [("bf16", 128, 16), ("bf16", 64, 64), ("bf16", 128, 64), ("f32", 64, 16), ("f32", 128, 40)])
+def test_whole_dense_cache_is_the_plain_call(dtype, d, n, tree):
+    """A dense cache without a window: the plain entry point's bits, also where the softmax's reference moves often."""
+    for lens, sharp in (([1300, 77, 0], 8.0), ([2600], 1.0)):
+        c = Case(dtype, "dense", d, n, 28, 4, lens, seed=51, sharp=sharp, poison=True)
+        got = c.attn(tree)
+        args = [t.cuda() for t in (c.q, c.cache.k, c.cache.v, c.k_new, c.v_new, c.cache.ctx_lens)]
+        want = G.glance_tree_verify_attn(*args, c.parents.cuda()) if tree else G.glance_block_draft_attn(*args)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (lens, sharp)
