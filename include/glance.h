@@ -373,10 +373,10 @@ glance_status glance_build_tree(int32_t batch, int32_t horizon, int32_t vocab, i
  * Row i of a block is at position ctx + i, a tree's node at ctx + its depth.
  * Of the new keys a block's rows see all (the block stays bidirectional within
  * itself), a tree's rows see their ancestors at positions that satisfy the same
- * condition, and every row sees itself.  Context that no row of a call sees is
- * not read, whatever it holds.  A key or value that some row sees has to be
- * finite: a NaN or infinity in it may reach other rows of the same sequence and
- * KV head.
+ * condition, and every row sees itself.  Context that no row of a call sees has no
+ * part in its results, whatever it holds (the attention does not read it, the
+ * weights read some of it).  A key or value that some row sees has to be finite:
+ * a NaN or infinity in it may reach other rows of the same sequence and KV head.
  */
 typedef enum { GLANCE_CACHE_DENSE = 0, GLANCE_CACHE_KV4 = 1 } glance_cache_format;
 

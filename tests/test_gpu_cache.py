@@ -652,3 +652,233 @@ def test_whole_dense_cache_is_the_plain_call(dtype, d, n, tree):
         want = G.glance_tree_verify_attn(*args, c.parents.cuda()) if tree else G.glance_block_draft_attn(*args)
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), (lens, sharp)
+
+
+# ------------------------------------------------------------- values and calls at the edges
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_codes_of_the_smallest_values(dtype, d):
+    """Around 2^-127, half the smallest code's value at the least exponent, inputs are subnormal: those above it
+    round to a code that is not 0."""
+    g = torch.Generator().manual_seed(d)
+    rows = 96
+    x = torch.exp2(torch.rand(rows, d, generator=g).double() * 10 - 131)  # 2^-131 .. 2^-121
+    x[:32] = x[:32].clamp(max=2.0 ** -126)                                # blocks of subnormals alone
+    step = 2.0 ** -133 if dtype == "bf16" else 2.0 ** -149                # of the type's subnormals
+    at = torch.tensor([2.0 ** -127 + i * step for i in (-1, 0, 1)] + [2.0 ** -126, 2.0 ** -126 - step, step, 3 * 2.0 ** -127, 2.0 ** -125])
+    x[0, :8], x[1, :8], x[40, 8:16] = at, at[:1], at
+    x = torch.where(torch.rand(rows, d, generator=g) < 0.5, x, -x).to(DT[dtype])
+    assert (x != 0).sum() > x.numel() // 2 and (x.double().abs() < 2.0 ** -126).any()
+    codes, scales = OC.encode(x.double())
+    assert (((codes & 7) == 1) & (x.double().abs().numpy() < 2.0 ** -126)).any()
+    src = G.ContextCache(x.reshape(1, 2, -1, d).cuda(), x.flip(0).reshape(1, 2, -1, d).cuda(),
+                         torch.tensor([rows // 2], dtype=torch.int32).cuda())
+    packed, back = G.new_cache(1, 2, rows // 2, d, fmt="kv4"), G.new_cache(1, 2, rows // 2, d, dtype=DT[dtype])
+    G.glance_cache_convert(src, packed)
+    G.glance_cache_convert(packed, back)
+    # committed rows are rounded alike: rows 0 .. 31 of head 0 as 32 nodes of one KV head
+    into = G.new_cache(1, 1, 32, d, fmt="kv4")
+    new = x[:32].reshape(1, 32, 1, d).cuda()
+    path = torch.arange(32, dtype=torch.int32)[None].cuda()
+    G.glance_cache_commit_path(into, new, new, torch.tensor([31], dtype=torch.int32).cuda(), path)
+    torch.cuda.synchronize()
+    for name, ref, sc in (("k", codes, scales), ("v", codes[::-1], scales[::-1])):
+        assert np.array_equal(getattr(packed, name + "_scale").cpu().numpy().reshape(rows, -1), sc)
+        assert np.array_equal(getattr(packed, name).cpu().numpy().reshape(rows, -1), OC.pack(ref))
+        np.testing.assert_array_equal(_np(getattr(back, name)).reshape(rows, d), OC.decode(OC.pack(ref), sc).astype(np.float32))
+    assert np.array_equal(into.k.cpu().numpy().reshape(32, -1), OC.pack(codes[:32]))
+    assert np.array_equal(into.v_scale.cpu().numpy().reshape(32, -1), scales[:32])
+
+
+def _weigh_close(c, got, lse, ref, rows, upto, cap_fill=None):
+    c.k64 = np.nan_to_num(c.k64)  # (what no row sees enters no weight)
+    for b, end in enumerate(upto):
+        bound = _weight_bound(c, lse.numpy(), rows, ref[b, :, :end])
+        assert (np.abs(got[b, :, :end] - ref[b, :, :end]) <= bound).all(), (b, np.abs(got[b, :, :end] - ref[b, :, :end]).max())
+        if cap_fill is not None:
+            assert (got[b, :, end:] == cap_fill).all()
+
+
+@pytest.mark.parametrize("n_sinks,window", [(0, 1), (3, 1), (5, 40), (70, 100), (1, 190)])
+@pytest.mark.parametrize("fmt,dtype,d", [("dense", "bf16", 128), ("kv4", "bf16", 64), ("dense", "f32", 64), ("kv4", "f32", 128)])
+def test_weights_do_not_depend_on_unseen_slots(fmt, dtype, d, n_sinks, window):
+    """NaN in every slot that no row sees: those slots only fade."""
+    lens = [0, 1, 40, 64, 65, 200, 321]
+    c = Case(dtype, fmt, d, 9, 4, 2, lens, cap=330, seed=window + d, poison=True, n_sinks=n_sinks, window=window, weights=True)
+    lse = torch.tensor(c.want(False, n_sinks, window)[1], dtype=torch.float32)
+    into = torch.full_like(c.cache.weights, 7.0)
+    got = G.glance_cache_weigh(c.q.cuda(), c.cache, lse.cuda(), decay=0.5, n_sinks=n_sinks, window=window, weights_out=into).cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        ref = OC.weigh(c.q.double(), c.k64, lse.double(), c.lens, c.weights.double(), 0.5, n_sinks=n_sinks, window=window)
+    assert np.isfinite(ref).all()
+    _weigh_close(c, got, lse, ref, 18, lens, 7.0)
+
+
+@pytest.mark.parametrize("n_sinks,window", [(0, 0), (5, 40)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fmt,dtype", [("dense", "bf16"), ("kv4", "bf16"), ("dense", "f32"), ("kv4", "f32")])
+def test_weights_of_the_longest_path(fmt, dtype, d, n_sinks, window):
+    """A path of 64 nodes of 14 heads: more rows than a workgroup holds at a time, and slots-to-be past the capacity."""
+    lens, cap = [300, 0, 680], 700
+    c = Case(dtype, fmt, d, 64, 14, 1, lens, cap=cap, seed=d, weights=True)
+    c.parents = torch.arange(-1, 63, dtype=torch.int32).repeat(3, 1)
+    lse = torch.tensor(c.want(True, n_sinks, window)[1], dtype=torch.float32)
+    alen, path = torch.tensor([63, 63, 2 ** 31 - 1], dtype=torch.int32), torch.arange(64, dtype=torch.int32).repeat(3, 1)
+    into = torch.full_like(c.cache.weights, 7.0)
+    got = G.glance_cache_weigh(c.q.cuda(), c.cache, lse.cuda(), c.k_new.cuda(), alen.cuda(), path.cuda(), 0.5, n_sinks, window, into).cpu().numpy()
+    ref = OC.weigh(c.q.double(), c.k64, lse.double(), c.lens, c.weights.double(), 0.5, c.k_new.double().numpy(), alen.numpy(), path.numpy(),
+                   n_sinks, window)
+    _weigh_close(c, got, lse, ref, 64 * 14, [364, 64, cap], 7.0)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("dense", "bf16"), ("kv4", "f32")])
+def test_weights_from_none(fmt, dtype):
+    """With decay 0 the cache needs no weights; without any an output has to be given."""
+    c = Case(dtype, fmt, 64, 5, 4, 2, [90, 3], seed=8)
+    lse = torch.tensor(c.want(False)[1], dtype=torch.float32)
+    with pytest.raises(ValueError, match="weights"):
+        G.glance_cache_weigh(c.q.cuda(), c.cache, lse.cuda(), decay=0.0)
+    into = torch.full((2, 2, 90), float("nan")).cuda()
+    with pytest.raises(G.GlanceError, match="weights"):
+        G.glance_cache_weigh(c.q.cuda(), c.cache, lse.cuda(), decay=0.5, weights_out=into)
+    got = G.glance_cache_weigh(c.q.cuda(), c.cache, lse.cuda(), decay=0.0, weights_out=into).cpu().numpy()
+    ref = OC.weigh(c.q.double(), c.k64, lse.double(), c.lens, np.zeros((2, 2, 90)), 0.0)
+    _weigh_close(c, got, lse, ref, 10, [90, 3])
+    assert np.isnan(got[1, :, 3:]).all()
+
+
+@pytest.mark.parametrize("fmt", ["dense", "kv4"])
+def test_every_call_clamps_lengths(fmt):
+    """Lengths below 0 and past the capacity give what 0 and the capacity give."""
+    outs = []
+    for lens in ([120, 0, 64], [10 ** 9, -5, 64]):
+        c = Case("bf16", fmt, 64, 4, 4, 2, [120, 0, 64], cap=120, seed=17, weights=True)
+        c.cache.ctx_lens = torch.tensor(lens, dtype=torch.int32).cuda()
+        q, kn, vn = c.q.cuda(), c.k_new.cuda(), c.v_new.cuda()
+        lse = torch.ones(3, 4, 4).cuda()
+        got = [G.glance_cache_weigh(q, c.cache, lse, decay=0.5, n_sinks=3, window=50, weights_out=torch.zeros(3, 2, 120).cuda())]
+        to = G.new_cache(3, 2, 70, 64, fmt=fmt, weights=True)
+        got += [G.glance_cache_evict(c.cache, to, 70, 3, 5), to.k, to.v, to.weights, to.ctx_lens]
+        other = G.new_cache(3, 2, 100, 64, fmt="dense" if fmt == "kv4" else "kv4")
+        G.glance_cache_convert(c.cache, other)
+        got += [other.k, other.v, other.ctx_lens]
+        path = torch.tensor([[0, 2, -1]] * 3, dtype=torch.int32).cuda()
+        G.glance_cache_commit_path(c.cache, kn, vn, torch.tensor([1, 1, 1], dtype=torch.int32).cuda(), path)
+        got += [c.cache.k, c.cache.v, c.cache.ctx_lens]
+        torch.cuda.synchronize()
+        outs.append(got)
+    assert outs[1][5].cpu().tolist() == [70, 0, 64] and outs[1][-1].cpu().tolist() == [120, 2, 66]
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", ["dense", "kv4"])
+def test_calls_on_another_stream_give_the_same(fmt):
+    """Every call that takes a stream, on one of its own: the bits of the same calls on the current stream."""
+    def results(stream):
+        c = Case("bf16", fmt, 64, 8, 4, 2, [300, 200], cap=320, seed=30, weights=True)
+        q, kn, vn, par = c.q.cuda(), c.k_new.cuda(), c.v_new.cuda(), c.parents.cuda()
+        alen = torch.tensor([2, 1], dtype=torch.int32).cuda()
+        path = torch.tensor([[0, 1, 2], [0, 1, -1]], dtype=torch.int32).cuda()
+        into = torch.zeros_like(c.cache.weights)
+        to = G.new_cache(2, 2, 128, 64, fmt=fmt, weights=True)
+        other = G.new_cache(2, 2, 320, 64, fmt="dense" if fmt == "kv4" else "kv4")
+        torch.cuda.synchronize()  # all of it is there before a stream of the calls' own starts
+        out, lse = G.glance_cache_tree_verify_attn(q, c.cache, kn, vn, par, 2, 100, stream=stream)
+        draft = G.glance_cache_block_draft_attn(q, c.cache, kn, vn, stream=stream)
+        G.glance_cache_weigh(q, c.cache, lse, kn, alen, path, 0.5, 2, 100, weights_out=into, stream=stream)
+        G.glance_cache_commit_path(c.cache, kn, vn, alen, path, stream=stream)
+        kept = G.glance_cache_evict(c.cache, to, 128, 2, 16, stream=stream)
+        G.glance_cache_convert(c.cache, other, stream=stream)
+        torch.cuda.synchronize()
+        return [out, lse, *draft, into, c.cache.k, c.cache.ctx_lens, kept, to.k, to.v, to.weights, to.ctx_lens, other.k, other.v,
+                other.ctx_lens]
+
+    want = results(None)
+    assert (want[4] > 0).any()
+    for a, b in zip(results(torch.cuda.Stream()), want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", ["dense", "kv4"])
+def test_rounds_on_a_stream_of_their_own(fmt):
+    with torch.cuda.stream(torch.cuda.Stream()):
+        _rounds(fmt, "bf16", rounds=2)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_conversion_and_commit_captured(dtype):
+    """A prepared conversion both ways and a commit between them, replayed with other work between the replays."""
+    c = Case(dtype, "dense", 64, 6, 2, 2, [40, 9], cap=48, seed=41)
+    kn, vn = c.k_new.cuda(), c.v_new.cuda()
+    alen, path = torch.tensor([2, 0], dtype=torch.int32).cuda(), torch.tensor([[0, 3, 5], [1, -1, -1]], dtype=torch.int32).cuda()
+    side = torch.cuda.Stream()
+    packed, back = G.new_cache(2, 2, 48, 64, fmt="kv4"), G.new_cache(2, 2, 48, 64, dtype=DT[dtype])
+    pack, unpack = (G.prepare_cache_convert(a, b, stream=side) for a, b in ((c.cache, packed), (packed, back)))
+    state = [packed.k, packed.v, packed.k_scale, packed.v_scale, packed.ctx_lens, back.k, back.v, back.ctx_lens]
+
+    def run():
+        pack()
+        G.glance_cache_commit_path(packed, kn, vn, alen, path, stream=side)
+        unpack()
+
+    torch.cuda.synchronize()
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in state]
+    assert want[4].cpu().tolist() == [43, 10]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for _ in range(3):
+        for t in state:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(state, want):
+            assert torch.equal(a, b)
+        run()
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["dense", "kv4"])
+def test_evict_past_32_bits_from_every_head(fmt):
+    """Kept slots over a whole cache of more than 4 GB a side: each head's known ones, in order, with their rows."""
+    hkv, cap, d, some, sinks, recent = (2, 2 ** 24 + 3, 128, 300, 8, 12) if fmt == "dense" else (4, 2 ** 25, 128, 300, 8, 12)
+    rng = np.random.default_rng(1)
+    slots = [np.sort(rng.permutation(np.unique(rng.integers(sinks, cap - recent, 2 * some)))[:some]) for _ in range(hkv)]
+    src = G.new_cache(1, hkv, cap, d, fmt=fmt, weights=True)
+    src.ctx_lens.fill_(cap)
+    want = []
+    for g in range(hkv):
+        at = torch.tensor(slots[g]).cuda()
+        src.weights[0, g, at] = torch.arange(1, some + 1, dtype=torch.float32).cuda()
+        keep = np.concatenate([np.arange(sinks), slots[g], np.arange(cap - recent, cap)])
+        want.append(keep.tolist())
+        at = torch.tensor(keep).cuda()
+        for i, t in enumerate((src.k, src.v)):  # rows that tell their slot and side
+            t[0, g, at, :4] = torch.stack([(at >> s) % 16 + i for s in (0, 4, 8, 12)], -1).to(t.dtype)
+    to = G.new_cache(1, hkv, some + sinks + recent, d, fmt=fmt, weights=True)
+    kept = G.glance_cache_evict(src, to, some + sinks + recent, sinks, recent)
+    torch.cuda.synchronize()
+    assert to.ctx_lens.item() == some + sinks + recent
+    for g in range(hkv):
+        assert kept[0, g].cpu().tolist() == want[g]
+        at = torch.tensor(want[g]).cuda()
+        for t, s in ((to.k, src.k), (to.v, src.v), (to.weights, src.weights)):
+            assert torch.equal(t[0, g], s[0, g, at])
+
+
+@pytest.mark.parametrize("fmt,n_sinks,window", [("dense", 4, 1500), ("dense", 0, 0), ("kv4", 0, 0), ("kv4", 9, 700)])
+@pytest.mark.parametrize("n", [1, 16, 64])
+def test_bf16_outputs_err_by_two_roundings(fmt, n_sinks, window, n):
+    """Probabilities are rounded to bf16 before P.V and outputs once more.  Derived: with values independent of mean 0
+    an output is sqrt(sum w^2) of theirs in size and the error of the first rounding at most 2^-8 / sqrt(3) of that
+    (each probability's error is spread over half a step either way, at most 2^-8 of it), of the second the same, of a
+    piece's fp16 2^-11 / sqrt(3): the root of their squares is 3.2e-3.  Nothing else enters."""
+    c = Case("bf16", fmt, 128, n, 28, 4, [2048, 1777], seed=60 + n)
+    out, _ = c.attn(True, n_sinks, window)
+    ref = c.want(True, n_sinks, window)[0]
+    assert np.sqrt(((_np(out) - ref) ** 2).mean() / (ref ** 2).mean()) < 3.3e-3
