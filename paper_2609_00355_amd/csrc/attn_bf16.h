@@ -10,8 +10,10 @@
 // are planned on the device from ctx_lens, the same way by every workgroup:
 // each sequence of len_b tiles gets n_b = ceil(len_b / T) pieces of nearly
 // equal size, with T the smallest size for which all pieces fit the launched
-// slots; so a ragged batch gets pieces of equal cost rather than equal key
-// ranges, and no slot is spent on a sequence's padding.
+// slots; so a ragged batch's pieces follow its lengths, and no slot is spent on a
+// sequence's padding.  No piece crosses a sequence's end, so with few slots a
+// sequence they are uneven: of 16 contexts of 2048 to 32768 keys, 32 slots a
+// head (64 rows of 28/4 heads), the longest piece has 174 tiles, the mean 139.
 //
 // Waves.  Waves 0 .. tiles-1 compute one 32-row tile each.  The waves
 // without rows (one to four of them issue) stream K/V tiles from HBM straight
@@ -44,11 +46,21 @@
 // first keys: 31.6 us, 26.3 for its bytes at the rate of a large copy (bound by
 // memory).  64 rows, the same window, 64 first keys, 4 sequences: 30.5, 12.4 for its products at the
 // rate of a large matrix product: start-up 6, eight tiles of 1.7, the merge 6.
-// 4-bit caches: 16 rows over 4 x 16384 keys 27.5 (a dense cache: 36 to 40), 12.2 for
+// 4-bit caches: 16 rows over 4 x 16384 keys 27.5 (a dense cache: 40), 12.2 for
 // its products: 16 tiles of 1.0, bound by the vector instructions of the softmax and
 // by LDS, of which the operands take 1300 and the conversion's stores 400 cycles of
-// a tile's 2150; 64 rows over 16 ragged caches 284, 211 for its products: the one
-// converting wave takes 3450 cycles a tile, which the computing waves need as well.
+// a tile's 2150; 64 rows over 16 ragged caches 287, 211 for its products: the one
+// converting wave takes 3450 cycles a tile, which the computing waves need as well,
+// and the longest piece, which decides, is a quarter above the mean.  One row over
+// these caches 81, 31 for its bytes: a single wave computes, its tiles one after
+// another.
+//
+// Roundings.  The matrix unit multiplies bf16 by bf16, so a probability is rounded
+// to bf16 (by at most 2^-8 of it) before P.V, and the row's sum is taken of the
+// rounded ones, so that they still weigh the values.  The errors are independent:
+// an output over many keys is off by 1.65e-3 of its size (root mean square), as
+// much as the output's own rounding adds; 2.3e-3 together.  fp16 probabilities (an
+// eighth of that) would need the values in fp16, whose range bf16 values exceed.
 //
 // Merge.  A piece that is its sequence's only one writes the output and LSE.
 // Otherwise each piece writes its normalised output in fp16 (in the MFMA
@@ -863,8 +875,12 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     };
     int t = 1;
     // Where the steps' code begins within a 64-byte line matters with seven
-    // computing waves: 16 ragged verifies of up to 32768 keys in a round took
-    // 468 us with the first step's barrier at byte 40, 477 at 52, 475 at 48.
+    // computing waves: 64 rows over 16 ragged contexts of up to 32768 keys take 297
+    // us with this padding and 304 without it or with the alignment alone (three
+    // runs of each in turn, each within 1 of these); over 4 x 16384 keys no
+    // difference.  The padding suits the code that the compiler puts behind it now
+    // and nothing checks that: after a change to this kernel, or of the compiler,
+    // it has to be timed against none again.
     if constexpr (D == 128 && TREE && WIDE) asm volatile(".p2align 6\n\t.rept 14\n\ts_nop 0\n\t.endr");
     while (t < n_tiles) {
       step(t, I1{});

@@ -7,16 +7,21 @@
 //
 // Selection, by a workgroup of a (sequence, KV head): the least kept weight by
 // counts of order-preserving keys, then the kept slots in order by prefix sums.
-// Bound by latency: one read of the weights and about a dozen barriers.  Then the kept rows of K, V, scales
-// and weights are copied, 16 bytes a lane, bound by memory.
+// Bound by the instructions of some five passes over a workgroup's keys and a dozen
+// barriers.  Then the kept rows of K, V, scales and weights are copied, 16 bytes a
+// lane, bound by memory.
 //
 // Where LDS holds every key of the cache, the workgroups of a head (as many as
 // fill the compute units) all select, which costs no more time than one doing so,
-// and each copies its share of the rows: one launch.  Longer caches' selection
-// reads the weights several times: one workgroup does it and a second launch
-// copies.  4096 of 16384 slots of 16 heads of 128 in bf16 (33 MB kept): 21.3 us in
-// one launch, the selection 10 of it, 26.0 in two (13.7 at the rate of a large
-// copy); 5001 of up to 11003 slots of 10 fp32 heads of 64: 16.0, 21.1.
+// and each copies its share of the rows: one launch.  The lengths are not known
+// when the launch is chosen, so the capacity decides.  Caches of larger capacity:
+// one workgroup a head selects, reading the weights past the held ones in
+// every pass, and a second launch copies.  4096 of 16384 slots of 16 heads of 128 in
+// bf16 (33 MB kept): 21.3 us in one launch, the selection 10 of it (13.7 at the rate
+// of a large copy), 23.7 in two; 5001 of up to 11003 slots of 10 fp32 heads of 64:
+// 16.0 and 19.9 (9.7).  Beyond, the selection grows with the length: a quarter of
+// 65536, 131072 and 262144 slots of 4 bf16 heads of 128 takes 41, 82 and 157 us
+// (13.7, 27.4 and 54.8), of 16 such heads 85, 159 and 310 (55, 110 and 219).
 #include "glance_internal.h"
 
 #include "attn_plan.h"

@@ -5,17 +5,21 @@
 // rows being (new row, query head of the group) pairs: all of a block's, or those
 // of an accepted path.  The scores are formed again from the queries, the keys
 // and the call's log-sum-exps; with those known a slot's sum needs no other
-// slot, so every tile of 32 KB keys belongs to one wave, which walks all rows:
-// no second pass, no atomics, the same bits every time.
+// slot, so every tile of 32 KB keys belongs to one wave, which walks the rows: no
+// atomics, the same bits every time, and one pass over the keys where the rows
+// fit LDS (below).
 //
-// Work.  The context tiles of 64 keys that some row sees are cut into pieces of
-// equal size by the attention's plan (attn_plan.h), a workgroup each, about one a
-// compute unit; its waves take the piece's tiles as they become free (a wave
-// that shares its SIMD with an older one gets two thirds of its turns).  Slots
-// that no row sees only fade, and the pieces of their sequence share them.  The
-// queries of up to kRows rows are staged in LDS once a workgroup (more rows: in
-// turn, the sums added up in the output), a tile's keys are loaded into registers
-// while the tile before is computed.
+// Work.  The context tiles of 64 keys that some row sees are cut into pieces by
+// the attention's plan (attn_plan.h; equal within a sequence, and over 16 ragged
+// contexts of 2048 to 32768 keys at most 78 tiles, 70 on average), a workgroup
+// each, about one a compute unit; its waves take the piece's tiles as they become
+// free (a wave that shares its SIMD with an older one gets two thirds of its
+// turns).  Slots that no row sees only fade, and the pieces of their sequence share
+// them.  The queries of up to kRows rows, 256 or, in fp32 with 128 dims, 128, are
+// staged in LDS; more rows come in turn, for which the keys are read, converted
+// and the sums read back again (64 rows of 7 heads over 4 x 16384 bf16 keys: two
+// turns, 50 us; over 4-bit keys 38).  A tile's keys are loaded into registers while
+// the tile before is computed.
 //
 // S[row][key] = Q . K^T with the rows as matrix operand A: a lane's results are
 // 16 rows of one key, so the sums over rows are sums over a lane's registers
@@ -442,8 +446,14 @@ hipError_t launch_weigh(const WeighParams& params, bool bf16, hipStream_t s, hip
   p.plan.window = p.window;
   const int per_g = 256 / p.hkv;
   p.plan.slots_per_g = per_g > p.batch ? per_g : p.batch;
+  // The least piece is the attention's rule (least_piece(), here up to four tiles),
+  // which is one of its merge; there is none here.  It costs where workgroups would
+  // be left over, above all in fp32, whose waves share a step only in pieces of one
+  // or two tiles: with the rule, and with pieces of one tile, 64 rows of 12/1 heads
+  // of 128 over 4096 fp32 keys take 122 and 60 us, 16 rows of 28/4 heads 23.7 and
+  // 16.3; in bf16 24.9 and 23.0, 9.2 and 9.2; full calls the same.
   p.plan.min_tiles = 1;
-  p.plan.tiles_rg = 5;  // (least_piece: no more than four)
+  p.plan.tiles_rg = 5;
   if (ev0) (void)hipEventRecord(ev0, s);
   if (p.d == 128) {
     if (bf16) launch<128, true>(p, s);
