@@ -877,7 +877,7 @@ __global__ __launch_bounds__(512) void attn_bf16(AttnParams p) {
     // Where the steps' code begins within a 64-byte line matters with seven
     // computing waves: 64 rows over 16 ragged contexts of up to 32768 keys take 297
     // us with this padding and 304 without it or with the alignment alone (three
-    // runs of each in turn, each within 1 of these); over 4 x 16384 keys no
+    // runs of each in turn, each within 2 of these); over 4 x 16384 keys no
     // difference.  The padding suits the code that the compiler puts behind it now
     // and nothing checks that: after a change to this kernel, or of the compiler,
     // it has to be timed against none again.
